@@ -88,6 +88,7 @@ def draw(rng):
     if G in (2, 4, 8) and rng.random() < 0.3:
         c["tq"] = rng.choice([2, 4, 5])
         c["Hq"] *= c["tq"]
+        c["scores"] = False              # (of drafts they are the library's own, in its order of rows)
     elif rng.random() < 0.2:
         c["per_head"] = True
     heads = c["Hq"] if c["per_head"] else c["Hkv"]
