@@ -372,6 +372,95 @@ int pikv_policy_compact(const pikv_desc *desc, const int32_t *evicted_idx, const
                         int32_t max_evict, const int32_t *n_valid, int32_t *birth,
                         int32_t *last_access, int32_t *freq, void *stream);
 
+/* Queries and keys of new tokens out of a fused projection: the norm of each head, then the position
+ * rotation, in one pass (Algorithm 1 takes K_t, V_t and q_t as given; "K is stored post-rotation" in
+ * every call above).  Per token t and head, x its D values:
+ *     z = x * w / sqrt(mean(x^2) + eps)             (w = w_q or w_k, shared by the heads; NULL: z = x)
+ *     angle_i = positions[t] * inv_freq[i], i < rotary_dim / 2, not rounded below 64 bits
+ *     (z_a, z_b) -> (z_a cos - z_b sin, z_b cos + z_a sin) on the pairs (i, i + rotary_dim / 2), or
+ *     (2 i, 2 i + 1) with `interleaved`; values from rotary_dim on stay z
+ * in fp32, rounded once to the storage type.
+ *   x         [tokens] rows, `token_stride` elements apart (>= the row; a multiple of 16 bytes), each the
+ *             Hq query heads, then the Hkv key heads, then - if v_out - the Hkv value heads, D values each
+ *   w_q, w_k  [D] dtype or NULL (each for itself)
+ *   positions [tokens] int32;  inv_freq [rotary_dim / 2] float32: both may be NULL if rotary_dim == 0
+ *   q_out [tokens, Hq, D], k_out [tokens, Hkv, D], v_out [tokens, Hkv, D] dtype out: what pikv_route,
+ *             the appends and the attention calls take.  v_out may be NULL: no value heads are read.
+ *             Outputs must not overlap x or each other.
+ * Hq or Hkv may be 0 (separate projections); q_out or k_out may then be NULL.
+ * Errors: INVALID for null required pointers, tokens < 0, Hq or Hkv < 0 or both 0, token_stride too
+ * small, x, weights or outputs that are not 16-byte aligned, rotary_dim not in 0..D or no multiple of 16, eps < 0 or
+ * not finite, unknown dtype; UNSUPPORTED for D other than 16, 32, 64, 128 and for more than 2^23 blocks
+ * (tokens * heads / 16 of 128 values).  tokens == 0 is a no-op.                                           */
+int pikv_norm_rope(const void *x, int32_t tokens, int64_t token_stride, int32_t Hq, int32_t Hkv, int32_t D,
+                   int32_t dtype, const void *w_q, const void *w_k, float eps, const int32_t *positions,
+                   const float *inv_freq, int32_t rotary_dim, int32_t interleaved, void *q_out, void *k_out,
+                   void *v_out, void *stream);
+
+/* ---- The cache held in 8 bits ----
+ * Shards as above, but a row is D codes of one byte: desc->stride_h and desc->stride_s count bytes
+ * (rows still start on 16-byte boundaries) and desc->dtype is the type of the dense side (q, K_new, V_new, dense
+ * shards).  D is 32, 64 or 128 and rank 0 (UNSUPPORTED otherwise).
+ *   format  pikv_quant_format; block: 16, 32, 64 or 128 slots that share a scale
+ *   K_scales, V_scales [B,E,Hkv,ceil(S/block)] float32: one scale per block of slots
+ *           and kv head, K and V apart.  Entry i of a row stands for code_i * scale.
+ * Scales are powers of two: the smallest one, 2^-126 at the least, that brings the largest magnitude of
+ * the block's rows within the largest code (127 or 448).  Divisions by it are then exact, a code is the nearest
+ * one (ties to even) to x / scale, and the value it stands for is exact in either dense type unless that underflows
+ * - every call here gives the same bits on every machine.  A block that is given a NaN or an infinity has a NaN scale
+ * and reads as NaN until it is written anew.
+ * pikv_route, pikv_evict with compact == 0, pikv_policy_stamp, pikv_policy_utility and the utility updates serve these
+ * shards as they are; pikv_evict with compact != 0 moves rows of the dense type and must not be used
+ * on them, nor pikv_append, pikv_sharded_attn or the fused steps.                                                   */
+typedef enum { PIKV_QUANT_INT8 = 0, PIKV_QUANT_E4M3 = 1 } pikv_quant_format;
+
+/* Writes shards from dense ones: codes of the entries 0 .. n_valid[b][e]-1 (at most S) and the scales of the blocks
+ * they lie in; everything behind them is left as it was, and dense rows behind them are not read.
+ *   K_dense, V_dense  device tables of B*E shards of dtype, rows at h' * dense_stride_h + slot * dense_stride_s
+ *                     elements, on 16-byte boundaries
+ * Errors: descriptor errors, UNSUPPORTED as above and for 2^23 blocks of work or more (64 slots of a kv head's K or V
+ * each; 128 with block 128), INVALID for null pointers, unknown format, block other than the four, dense strides below D or
+ * not multiples of 16 bytes.  B == 0 is a no-op.                                                    */
+int pikv_quant_pack(const pikv_desc *desc, int32_t format, int32_t block, const void *const *K_dense,
+                    const void *const *V_dense, int64_t dense_stride_h, int64_t dense_stride_s,
+                    const int32_t *n_valid, void *const *K_shards, void *const *V_shards, float *K_scales,
+                    float *V_scales, void *stream);
+
+/* Reads them back: dense rows 0 .. n_valid[b][e]-1 = code * scale, rounded to the dense type; rows behind them are left
+ * as they were.  Arguments and errors as pikv_quant_pack.                                                     */
+int pikv_quant_read(const pikv_desc *desc, int32_t format, int32_t block, const void *const *K_shards,
+                    const void *const *V_shards, const float *K_scales, const float *V_scales,
+                    const int32_t *n_valid, void *const *K_dense, void *const *V_dense, int64_t dense_stride_h,
+                    int64_t dense_stride_s, void *stream);
+
+/* pikv_append for these shards: the same slot rule, utility and count; the new rows [B,Hkv,D] dtype become codes.  If
+ * other live slots share the block, its scale is the larger of its own and the one the new row needs, and where
+ * that is larger than its own their codes are rounded to it; else (the block's first entry) it is the new row's.  A
+ * scale does not shrink when the entry that set it leaves.  Live slots are those below n_valid + 1 or, with
+ * reuse_cnt[b][e] = c > 1 freed slots, below n_valid + c; no other row's codes are touched.
+ * Errors: descriptor errors, UNSUPPORTED as above, INVALID for null required pointers, unknown format or block,
+ * k not in 1..E, one of reuse_idx and reuse_cnt without the other, max_evict < 1 with them.  Per-token routing only
+ * (UNSUPPORTED otherwise).                                                                               */
+int pikv_quant_append(const pikv_desc *desc, int32_t format, int32_t block, const void *K_new, const void *V_new,
+                      const int32_t *topk_idx, int32_t k, const int32_t *reuse_idx, const int32_t *reuse_cnt,
+                      int32_t max_evict, void *const *K_shards, void *const *V_shards, float *K_scales,
+                      float *V_scales, float *utility, int32_t *n_valid, void *stream);
+
+/* Bytes of scratch pikv_quant_attn needs (host computation; 0 if the descriptor is invalid or not supported).
+ * The workspace must be 256-byte aligned.                                                                 */
+size_t pikv_quant_attn_workspace_bytes(const pikv_desc *desc, int32_t k);
+
+/* pikv_sharded_attn over these shards: same meaning of every argument, both combine modes, per-token and per-head
+ * routing; desc->tq > 1 (the multi-query layout above) for either dtype, every D here and any group size.  Scores and sums are
+ * those of the values code * scale, exact to fp32 accumulation.  scores + slot_coef feed pikv_update_utility.
+ * Errors: as pikv_sharded_attn; UNSUPPORTED as above, for tq > 1 with per-head routing, stride_s above 2^24 bytes and
+ * 2^23 blocks of work or more.                                                                   */
+int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t block, const void *q,
+                    const void *const *K_shards, const void *const *V_shards, const float *K_scales,
+                    const float *V_scales, const int32_t *n_valid, const int32_t *topk_idx, const float *gates,
+                    int32_t k, int32_t combine, float scale, float *y, float *row_max, float *row_norm,
+                    float *scores, float *slot_coef, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Tuning hook: force the number of row-range splits per (head group, selected shard) used
  * by pikv_sharded_attn and pikv_attn_workspace_bytes (process-wide; 0 restores the built-in
  * choice of one round of resident blocks).  Change it only between calls, and size the

@@ -25,13 +25,15 @@ COMBINE_LSE, COMBINE_LOCAL = 0, 1
 PENALTY_LOAD_BALANCE, PENALTY_CACHE_AWARE, PENALTY_ENTROPY = 0, 1, 2
 DESC_VALUE_BIAS = 1
 POLICY_H2O, POLICY_SL, POLICY_LRU, POLICY_LRU_PLUS = 0, 1, 2, 3
+QUANT_INT8, QUANT_E4M3 = 0, 1
 
 EXPORTS = ("pikv_route", "pikv_attn_workspace_bytes", "pikv_sharded_attn", "pikv_update_utility",
            "pikv_evict", "pikv_append", "pikv_strerror", "pikv_version", "pikv_set_attn_split", "pikv_decode_step",
            "pikv_stream_read_probe",
            "pikv_set_profile_events", "pikv_router_penalty", "pikv_compress", "pikv_policy_stamp",
            "pikv_update_utility_tracked", "pikv_policy_utility", "pikv_policy_compact", "pikv_decode_step_policy", "pikv_route_round_robin",
-           "pikv_sharded_attn_noalloc")
+           "pikv_sharded_attn_noalloc", "pikv_norm_rope", "pikv_quant_pack", "pikv_quant_read", "pikv_quant_append",
+           "pikv_quant_attn_workspace_bytes", "pikv_quant_attn")
 
 
 class PikvError(RuntimeError):
@@ -124,6 +126,20 @@ def load_library():
     lib.pikv_set_profile_events.restype = None
     lib.pikv_set_attn_split.argtypes = [i32]
     lib.pikv_set_attn_split.restype = None
+    i64 = C.c_int64
+    lib.pikv_norm_rope.argtypes = [vp, i32, i64, i32, i32, i32, i32, vp, vp, f32, vp, vp, i32, i32, vp, vp, vp, vp]
+    lib.pikv_norm_rope.restype = C.c_int
+    lib.pikv_quant_pack.argtypes = [dp, i32, i32, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp]
+    lib.pikv_quant_pack.restype = C.c_int
+    lib.pikv_quant_read.argtypes = [dp, i32, i32, vp, vp, vp, vp, vp, vp, vp, i64, i64, vp]
+    lib.pikv_quant_read.restype = C.c_int
+    lib.pikv_quant_append.argtypes = [dp, i32, i32, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.pikv_quant_append.restype = C.c_int
+    lib.pikv_quant_attn_workspace_bytes.argtypes = [dp, i32]
+    lib.pikv_quant_attn_workspace_bytes.restype = C.c_size_t
+    lib.pikv_quant_attn.argtypes = [dp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, f32,
+                                    vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.pikv_quant_attn.restype = C.c_int
     lib.pikv_version.argtypes = []
     lib.pikv_version.restype = C.c_int
     native = _load_native({name: C.cast(getattr(lib, name), C.c_void_p).value for name in EXPORTS})
@@ -461,3 +477,132 @@ def pikv_route_round_robin(rows, E, k, step, topk_idx, gates, stream=None):
     st = load_library().pikv_route_round_robin(rows, E, k, int(step), _p(topk_idx), _p(gates), _stream(stream))
     _check(st, "pikv_route_round_robin")
 
+
+# ---- Operators around an 8-bit cache.  What these pass on is checked here as well: the type of every tensor, and that all are
+# on one device, whose current stream they then use and which is current during the call.
+def _typed(where, want, *tensors):
+    for t in tensors:
+        if t is not None and t.dtype != want:
+            raise TypeError("%s: expected a tensor of %s, got %s" % (where, want, t.dtype))
+
+
+def _storage(desc):
+    import torch
+    return torch.float32 if desc.dtype == F32 else torch.bfloat16
+
+
+def _on_device(where, call, stream, *tensors):
+    """call(stream handle) with the tensors' device current."""
+    import torch
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("libpikv takes device memory only")
+        if device is not None and t.device != device:
+            raise ValueError("%s: tensors on %s and %s" % (where, device, t.device))
+        device = t.device
+    if device is None:
+        raise ValueError("%s: no tensor given" % where)
+    with torch.cuda.device(device):
+        return call(_stream(stream))
+
+
+def _int32_float32(where, integers, floats):
+    import torch
+    _typed(where, torch.int32, *integers)
+    _typed(where, torch.float32, *floats)
+
+
+def _rows(x, token_stride):
+    """Device address of rows that need not be contiguous: a slice of a wider projection."""
+    if (x.stride(-1) != 1 and x.shape[-1] > 1) or (x.dim() > 2 and x.stride(1) != x.shape[2]):
+        raise ValueError("the values of a row must be contiguous")
+    if x.dim() > 1 and not x.is_contiguous() and x.stride(0) != token_stride:
+        raise ValueError("rows are %d elements apart, token_stride is %d" % (x.stride(0), token_stride))
+    return x.data_ptr()
+
+
+def pikv_norm_rope(x, tokens, token_stride, Hq, Hkv, D, w_q, w_k, eps, positions, inv_freq, rotary_dim, interleaved, q_out,
+                   k_out, v_out=None, stream=None):
+    """``x``: [tokens, heads * D] or [tokens, heads, D], rows ``token_stride`` elements apart (a view into a wider projection is
+    taken as it is)."""
+    where = "pikv_norm_rope"
+    _typed(where, x.dtype, w_q, w_k, q_out, k_out, v_out)
+    st = _calls().pikv_norm_rope(x, tokens, token_stride, Hq, Hkv, D, w_q, w_k, eps, positions, inv_freq, rotary_dim,
+                                 1 if interleaved else 0, q_out, k_out, v_out, _raw(stream))
+    if st is None:
+        _int32_float32(where, [positions], [inv_freq])
+        st = _on_device(where, lambda s: load_library().pikv_norm_rope(
+            _rows(x, token_stride), tokens, token_stride, Hq, Hkv, D, _dtype_code(x), _p(w_q), _p(w_k), float(eps), _p(positions),
+            _p(inv_freq), rotary_dim, 1 if interleaved else 0, _p(q_out), _p(k_out), _p(v_out), s),
+            stream, x, w_q, w_k, positions, inv_freq, q_out, k_out, v_out)
+    if st != 0:
+        _check(st, where)
+
+
+def pikv_quant_pack(desc, format, block, K_dense, V_dense, dense_stride_h, dense_stride_s, n_valid, K_shards, V_shards, K_scales,
+                    V_scales, stream=None):
+    where = "pikv_quant_pack"
+    st = _calls().pikv_quant_pack(desc, format, block, K_dense, V_dense, dense_stride_h, dense_stride_s, n_valid, K_shards, V_shards,
+                                  K_scales, V_scales, _raw(stream))
+    if st is None:
+        _int32_float32(where, [n_valid], [K_scales, V_scales])
+        st = _on_device(where, lambda s: load_library().pikv_quant_pack(
+            C.byref(desc), format, block, _p(K_dense), _p(V_dense), dense_stride_h, dense_stride_s, _p(n_valid), _p(K_shards),
+            _p(V_shards), _p(K_scales), _p(V_scales), s), stream, K_dense, V_dense, n_valid, K_shards, V_shards, K_scales, V_scales)
+    if st != 0:
+        _check(st, where)
+
+
+def pikv_quant_read(desc, format, block, K_shards, V_shards, K_scales, V_scales, n_valid, K_dense, V_dense, dense_stride_h,
+                    dense_stride_s, stream=None):
+    where = "pikv_quant_read"
+    st = _calls().pikv_quant_read(desc, format, block, K_shards, V_shards, K_scales, V_scales, n_valid, K_dense, V_dense,
+                                  dense_stride_h, dense_stride_s, _raw(stream))
+    if st is None:
+        _int32_float32(where, [n_valid], [K_scales, V_scales])
+        st = _on_device(where, lambda s: load_library().pikv_quant_read(
+            C.byref(desc), format, block, _p(K_shards), _p(V_shards), _p(K_scales), _p(V_scales), _p(n_valid), _p(K_dense),
+            _p(V_dense), dense_stride_h, dense_stride_s, s), stream, K_shards, V_shards, K_scales, V_scales, n_valid, K_dense, V_dense)
+    if st != 0:
+        _check(st, where)
+
+
+def pikv_quant_append(desc, format, block, K_new, V_new, topk_idx, k, reuse_idx, reuse_cnt, max_evict, K_shards, V_shards, K_scales,
+                      V_scales, utility, n_valid, stream=None):
+    where = "pikv_quant_append"
+    _typed(where, _storage(desc), K_new, V_new)
+    st = _calls().pikv_quant_append(desc, format, block, K_new, V_new, topk_idx, k, reuse_idx, reuse_cnt, max_evict, K_shards,
+                                    V_shards, K_scales, V_scales, utility, n_valid, _raw(stream))
+    if st is None:
+        _int32_float32(where, [topk_idx, reuse_idx, reuse_cnt, n_valid], [K_scales, V_scales, utility])
+        st = _on_device(where, lambda s: load_library().pikv_quant_append(
+            C.byref(desc), format, block, _p(K_new), _p(V_new), _p(topk_idx), k, _p(reuse_idx), _p(reuse_cnt), max_evict,
+            _p(K_shards), _p(V_shards), _p(K_scales), _p(V_scales), _p(utility), _p(n_valid), s),
+            stream, K_new, V_new, topk_idx, reuse_idx, reuse_cnt, K_shards, V_shards, K_scales, V_scales, utility, n_valid)
+    if st != 0:
+        _check(st, where)
+
+
+def pikv_quant_attn_workspace_bytes(desc: PikvDesc, k: int) -> int:
+    return int(load_library().pikv_quant_attn_workspace_bytes(C.byref(desc), k))
+
+
+def pikv_quant_attn(desc, format, block, q, K_shards, V_shards, K_scales, V_scales, n_valid, topk_idx, gates, k, combine, scale, y,
+                    row_max, row_norm, scores, slot_coef, workspace, stream=None):
+    where = "pikv_quant_attn"
+    _typed(where, _storage(desc), q)
+    st = _calls().pikv_quant_attn(desc, format, block, q, K_shards, V_shards, K_scales, V_scales, n_valid, topk_idx, gates, k, combine,
+                                  scale, y, row_max, row_norm, scores, slot_coef, workspace, _raw(stream))
+    if st is None:
+        _int32_float32(where, [n_valid, topk_idx], [K_scales, V_scales, gates, y, row_max, row_norm, scores, slot_coef])
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        st = _on_device(where, lambda s: load_library().pikv_quant_attn(
+            C.byref(desc), format, block, _p(q), _p(K_shards), _p(V_shards), _p(K_scales), _p(V_scales), _p(n_valid), _p(topk_idx),
+            _p(gates), k, combine, float(scale), _p(y), _p(row_max), _p(row_norm), _p(scores), _p(slot_coef), _p(workspace), ws_bytes,
+            s), stream, q, K_shards, V_shards, K_scales, V_scales, n_valid, topk_idx, gates, y, row_max, row_norm, scores, slot_coef,
+            workspace)
+    if st != 0:
+        _check(st, where)

@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpikv.so")
 NATIVE = os.path.join(HERE, "_pikv_native.so")
 SOURCES = ["pikv_api.hip", "pikv_route.hip", "pikv_attn.hip", "pikv_utility.hip", "pikv_evict.hip", "pikv_step.hip", "pikv_aux.hip",
-           "pikv_policy.hip"]
+           "pikv_policy.hip", "pikv_rope.hip", "pikv_quant.hip", "pikv_quant_attn.hip"]
 
 # packed-fp32 instructions are switched off for all device code (the compiler would
 # otherwise form v_pk_*_f32 from ordinary float math)

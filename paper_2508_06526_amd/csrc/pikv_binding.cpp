@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -28,7 +29,7 @@ PyTypeObject *desc_type = nullptr, *policy_type = nullptr, *feedback_type = null
 // Addresses of the library's functions, in the order of `Functions`.
 enum Function {
     kRoute, kAttn, kAttnNoalloc, kUtility, kUtilityTracked, kEvict, kAppend, kStep, kStepPolicy, kCompress, kStamp, kPolicyUtility,
-    kPolicyCompact, kPenalty, kFunctions
+    kPolicyCompact, kPenalty, kNormRope, kQuantPack, kQuantRead, kQuantAppend, kQuantAttn, kFunctions
 };
 void *addresses[kFunctions] = {};
 
@@ -55,6 +56,7 @@ struct Args {
     const at::Tensor *last = nullptr;    // the last tensor taken
     const at::Tensor *first = nullptr;
     bool usual = true;                   // every argument so far was of the ordinary kind (no exception: one costs as much as a call)
+    bool strict = false;                 // the tensors of int32_t * and float * are of that type, and all are on one device
 
     template <typename T>
     T unusual() {
@@ -65,6 +67,7 @@ struct Args {
         if (o == Py_None) return nullptr;
         if (!THPVariable_CheckExact(o)) return unusual<const at::Tensor *>();
         const at::Tensor &t = THPVariable_Unpack(o);
+        if (strict && first != nullptr && t.device() != first->device()) return unusual<const at::Tensor *>();
         return t.is_cuda() && t.is_contiguous() ? &t : unusual<const at::Tensor *>();
     }
     template <typename T>
@@ -78,6 +81,7 @@ struct Args {
 struct Stream {};      // void *: the caller's, as an integer, or None - torch's current one
 struct Bytes {};       // size_t: of the tensor before it; takes no argument
 struct Dtype {};       // int32_t: of the first argument, a tensor; takes none itself
+struct DeviceStream {};      // void *: like Stream, torch's current one being that of the tensors' device; makes the call strict
 
 template <typename T, typename Kind>
 struct Take {
@@ -91,6 +95,10 @@ struct Take {
             return mine ? a.template buffer<T>(o) : a.template unusual<T>();
         } else if constexpr (std::is_pointer_v<T>) {
             const at::Tensor *t = a.tensor(o);
+            typedef std::remove_const_t<std::remove_pointer_t<T>> Element;
+            if (a.strict && t != nullptr && ((std::is_same_v<Element, int32_t> && t->scalar_type() != at::kInt) ||
+                                             (std::is_same_v<Element, float> && t->scalar_type() != at::kFloat)))
+                return a.template unusual<T>();
             a.last = t;
             if (a.first == nullptr) a.first = t;
             return t == nullptr ? nullptr : static_cast<T>(t->data_ptr());
@@ -104,7 +112,8 @@ struct Take {
             if (!PyLong_CheckExact(o) && !PyBool_Check(o)) return a.template unusual<T>();
             int overflow = 0;
             const long long v = PyLong_AsLongLongAndOverflow(o, &overflow);
-            return overflow == 0 && v >= INT32_MIN && v <= INT32_MAX ? static_cast<T>(v) : a.template unusual<T>();
+            const bool fits = sizeof(T) == 8 || (v >= INT32_MIN && v <= INT32_MAX);
+            return overflow == 0 && fits ? static_cast<T>(v) : a.template unusual<T>();
         }
     }
 };
@@ -114,7 +123,7 @@ struct Take<T, Stream> {
         PyObject *o = *a.at++;
         if (o == Py_None) {
             if (a.first == nullptr) return a.template unusual<T>();     // (a tensor on the GPU: the device is initialised)
-            return c10::hip::getCurrentHIPStream().stream();
+            return c10::hip::getCurrentHIPStream(a.strict ? a.first->device().index() : -1).stream();
         }
         if (!PyLong_CheckExact(o)) return a.template unusual<T>();
         void *p = PyLong_AsVoidPtr(o);
@@ -125,6 +134,8 @@ struct Take<T, Stream> {
         return p;
     }
 };
+template <typename T>
+struct Take<T, DeviceStream> : Take<T, Stream> {};
 template <typename T>
 struct Take<T, Bytes> {
     static T from(Args &a) {
@@ -157,6 +168,20 @@ struct KindOf<I, At<INDEX, KIND>, REST...> {
 template <typename KIND>
 constexpr int takes = std::is_same_v<KIND, Bytes> || std::is_same_v<KIND, Dtype> ? 0 : 1;
 
+template <typename ENTRY>
+constexpr bool on_device = false;
+template <int INDEX>
+constexpr bool on_device<At<INDEX, DeviceStream>> = true;
+
+// A device, current for the length of a call.
+struct OnDevice {
+    const int before;
+    explicit OnDevice(int device) : before(device == c10::hip::current_device() ? -1 : c10::hip::ExchangeDevice(device)) {}
+    ~OnDevice() {
+        if (before >= 0) c10::hip::ExchangeDevice(before);
+    }
+};
+
 template <Function F, typename FN, typename... KINDS>
 struct Caller;
 template <Function F, typename... A, typename... KINDS>
@@ -166,14 +191,24 @@ struct Caller<F, int (*)(A...), KINDS...> {
         constexpr int wanted = (0 + ... + takes<typename KindOf<(int)I, KINDS...>::type>);
         if (n != wanted || addresses[F] == nullptr || at::impl::torch_function_mode_enabled()) Py_RETURN_NONE;
         try {
+            constexpr bool strict = (false || ... || on_device<KINDS>);
             Args a{args, args};
+            a.strict = strict;
             // (braces: the arguments are taken from left to right)
             const std::tuple<A...> values{Take<A, typename KindOf<(int)I, KINDS...>::type>::from(a)...};
             if (!a.usual || a.first == nullptr) Py_RETURN_NONE;
             auto call = [&]() noexcept { return std::apply(reinterpret_cast<int (*)(A...)>(addresses[F]), values); };
+            auto call_there = [&] {
+                if constexpr (strict) {
+                    const OnDevice here(a.first->device().index());
+                    return call();
+                } else {
+                    return call();
+                }
+            };
             int status;
             Py_BEGIN_ALLOW_THREADS
-            status = call();
+            status = call_there();
             Py_END_ALLOW_THREADS
             return PyLong_FromLong(status);
         } catch (...) {                  // torch's own refusal: the general path reports it
@@ -210,6 +245,11 @@ PyMethodDef methods[] = {
     method<kPolicyUtility, decltype(&pikv_policy_utility), At<12, Stream>>("pikv_policy_utility"),
     method<kPolicyCompact, decltype(&pikv_policy_compact), At<8, Stream>>("pikv_policy_compact"),
     method<kPenalty, decltype(&pikv_router_penalty), At<9, Stream>>("pikv_router_penalty"),
+    method<kNormRope, decltype(&pikv_norm_rope), At<6, Dtype>, At<17, DeviceStream>>("pikv_norm_rope"),
+    method<kQuantPack, decltype(&pikv_quant_pack), At<12, DeviceStream>>("pikv_quant_pack"),
+    method<kQuantRead, decltype(&pikv_quant_read), At<12, DeviceStream>>("pikv_quant_read"),
+    method<kQuantAppend, decltype(&pikv_quant_append), At<16, DeviceStream>>("pikv_quant_append"),
+    method<kQuantAttn, decltype(&pikv_quant_attn), At<20, Bytes>, At<21, DeviceStream>>("pikv_quant_attn"),
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -1,0 +1,161 @@
+// Norms of queries and keys for each head and the position rotation, out of a fused projection.
+//
+//   norm_rope : a block takes heads of one token, D / 8 lanes a head, 8 values a lane (loaded and stored in 16-byte pieces).
+//               The sum of squares is joined by a butterfly over the head's lanes; the partner of a value in the rotation sits
+//               rotary_dim / 16 lanes away (or in the same lane, interleaved).  The angles of a token are the same for all of its
+//               heads: cosines and sines are formed once per block, behind the first request for rows, and kept in LDS.
+//
+// Angle = position * inv_freq: in fp32 the product of a far position is off by its own rounding (position 10^6: 0.03
+// radians), so it is formed in 64 bits, in revolutions, and only what is left after whole ones is rounded.
+#include "pikv_mfma_dev.h"
+
+#include <math.h>
+
+namespace pikv {
+namespace {
+
+struct RopeParams {
+    const void *x, *w_q, *w_k;
+    const int32_t *positions;
+    const float *inv_freq;
+    void *q_out, *k_out, *v_out;
+    int64_t token_stride;
+    FastDiv by_parts;
+    int Hq, Hkv, rotary, interleaved, heads, per_block;    // heads: of a token, in all; per_block: of them a block takes
+    float eps;
+};
+
+constexpr int kRopeThreads = 256;
+
+template <typename T, int D>
+__global__ __launch_bounds__(kRopeThreads) void norm_rope(RopeParams p) {
+    constexpr int LPR = D / 8, STEP = kRopeThreads / LPR, N = sizeof(T) / 2;      // lanes of a head, heads at once, 16-byte pieces of 8 values
+    __shared__ float cos_s[64], sin_s[64];
+    int part;
+    const int token = fast_divide(p.by_parts, blockIdx.x, &part);
+    const int tid = threadIdx.x, c = tid & (LPR - 1);
+    const int last = min(p.heads, (part + 1) * p.per_block);
+    const int half = p.rotary >> 1;
+    if (tid < half) {
+        const double turns = (double)p.positions[token] * (double)p.inv_freq[tid] * 0.15915494309189533577;      // 1 / (2 pi)
+        sincospif((float)(2.0 * (turns - rint(turns))), &sin_s[tid], &cos_s[tid]);
+    }
+    __syncthreads();
+    const T *row = static_cast<const T *>(p.x) + token * p.token_stride;
+    for (int head = part * p.per_block + tid / LPR; head < last; head += STEP) {
+        uint4 raw[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) raw[i] = load16(reinterpret_cast<const char *>(row + (int64_t)head * D + 8 * c) + 16 * i);
+        const bool key = head >= p.Hq && head < p.Hq + p.Hkv, value = head >= p.Hq + p.Hkv;
+        T *out;
+        if (value) out = static_cast<T *>(p.v_out) + ((int64_t)token * p.Hkv + head - p.Hq - p.Hkv) * D;
+        else if (key) out = static_cast<T *>(p.k_out) + ((int64_t)token * p.Hkv + head - p.Hq) * D;
+        else out = static_cast<T *>(p.q_out) + ((int64_t)token * p.Hq + head) * D;
+        out += 8 * c;
+        if (value) {                                  // copied as they are
+#pragma unroll
+            for (int i = 0; i < N; ++i) store16(reinterpret_cast<char *>(out) + 16 * i, raw[i]);
+            continue;
+        }
+        float z[8];
+#pragma unroll
+        for (int i = 0; i < N; ++i) Pack16<T>::widen(raw[i], z + i * Pack16<T>::N);
+        const T *w = static_cast<const T *>(key ? p.w_k : p.w_q);
+        if (w != nullptr) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(z[i], z[i], sum);
+#pragma unroll
+            for (int off = 1; off < LPR; off <<= 1) sum += __shfl_xor(sum, off, kWave);
+            const float r = 1.0f / sqrtf(sum * (1.0f / D) + p.eps);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = z[i] * r * load_scalar<T>(w, 8 * c + i);
+        }
+        if (8 * c < p.rotary) {                       // (rotary: a multiple of 16; a head's rotated lanes are whole pairs)
+            if (p.interleaved) {
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    const float cs = cos_s[4 * c + i / 2], sn = sin_s[4 * c + i / 2], a = z[i], b = z[i + 1];
+                    z[i] = a * cs - b * sn;
+                    z[i + 1] = b * cs + a * sn;
+                }
+            } else {
+                const bool second = 8 * c >= half;
+                const int lane = tid & (kWave - 1), other = second ? lane - half / 8 : lane + half / 8, i0 = second ? 8 * c - half : 8 * c;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float with = __shfl(z[i], other, kWave), cs = cos_s[i0 + i], sn = sin_s[i0 + i];
+                    z[i] = second ? z[i] * cs + with * sn : z[i] * cs - with * sn;
+                }
+            }
+        }
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                store16(out + 4 * i, make_uint4(__float_as_uint(z[4 * i]), __float_as_uint(z[4 * i + 1]), __float_as_uint(z[4 * i + 2]),
+                                                __float_as_uint(z[4 * i + 3])));
+        } else {
+            uint4 packed[1];
+            split_bf16(z, packed);
+            store16(out, packed[0]);
+        }
+    }
+}
+
+}  // namespace
+}  // namespace pikv
+
+using namespace pikv;
+
+extern "C" int pikv_norm_rope(const void *x, int32_t tokens, int64_t token_stride, int32_t Hq, int32_t Hkv, int32_t D,
+                              int32_t dtype, const void *w_q, const void *w_k, float eps, const int32_t *positions,
+                              const float *inv_freq, int32_t rotary_dim, int32_t interleaved, void *q_out, void *k_out,
+                              void *v_out, void *stream) {
+    if (tokens < 0 || Hq < 0 || Hkv < 0 || (Hq == 0 && Hkv == 0)) return PIKV_ERR_INVALID;
+    if (dtype != PIKV_F32 && dtype != PIKV_BF16) return PIKV_ERR_INVALID;
+    if (D != 16 && D != 32 && D != 64 && D != 128) return PIKV_ERR_UNSUPPORTED;
+    if (rotary_dim < 0 || rotary_dim > D || rotary_dim % 16 != 0) return PIKV_ERR_INVALID;
+    if (!(eps >= 0.0f) || eps > 3.0e38f) return PIKV_ERR_INVALID;
+    if (!x || (Hq > 0 && !q_out) || (Hkv > 0 && !k_out) || (rotary_dim > 0 && (!positions || !inv_freq))) return PIKV_ERR_INVALID;
+    const int64_t heads = (int64_t)Hq + (int64_t)Hkv * (v_out ? 2 : 1);
+    if (heads > (1 << 20)) return PIKV_ERR_UNSUPPORTED;
+    if (token_stride < heads * D || (token_stride * elem_bytes(dtype)) % 16 != 0) return PIKV_ERR_INVALID;
+    auto aligned = [](const void *ptr) { return reinterpret_cast<uintptr_t>(ptr) % 16 == 0; };
+    if (!aligned(x) || !aligned(w_q) || !aligned(w_k) || !aligned(q_out) || !aligned(k_out) || !aligned(v_out)) return PIKV_ERR_INVALID;
+    if (tokens == 0) return PIKV_OK;
+    RopeParams p;
+    p.x = x;
+    p.w_q = w_q;
+    p.w_k = w_k;
+    p.positions = positions;
+    p.inv_freq = inv_freq;
+    p.q_out = q_out;
+    p.k_out = k_out;
+    p.v_out = v_out;
+    p.token_stride = token_stride;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.rotary = rotary_dim;
+    p.interleaved = interleaved ? 1 : 0;
+    p.eps = eps;
+    p.heads = (int)heads;
+    const int at_once = kRopeThreads / (D / 8), passes = (p.heads + at_once - 1) / at_once;
+    const int parts = passes;
+    p.per_block = at_once;
+    p.by_parts = fast_div(parts);
+    if ((int64_t)tokens * parts > (1 << 23)) return PIKV_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)(tokens * parts));
+    auto launch = [&](auto type) {
+        typedef decltype(type) T;
+        hipStream_t st = as_stream(stream);
+        switch (D) {
+            case 16: hipLaunchKernelGGL((norm_rope<T, 16>), grid, dim3(kRopeThreads), 0, st, p); break;
+            case 32: hipLaunchKernelGGL((norm_rope<T, 32>), grid, dim3(kRopeThreads), 0, st, p); break;
+            case 64: hipLaunchKernelGGL((norm_rope<T, 64>), grid, dim3(kRopeThreads), 0, st, p); break;
+            default: hipLaunchKernelGGL((norm_rope<T, 128>), grid, dim3(kRopeThreads), 0, st, p); break;
+        }
+    };
+    if (dtype == PIKV_F32) launch(float{});
+    else launch(bf16{});
+    return launch_status();
+}
