@@ -25,8 +25,10 @@ namespace pikv {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kRows = 16;               // query rows of a block
-constexpr int kTile = 32;               // entries of a wave's pass
+constexpr int kRows = 16;               // query rows of a matrix tile
+constexpr int kTile = 32;               // entries of a stage of a wave
+constexpr int kMostTiles = 4;           // row tiles of a block
+constexpr int kLongestBlock = 1024;     // rows of a block, while the merge holds the partials
 
 struct QuantAttnParams {
     const void *q;
@@ -51,7 +53,7 @@ __device__ __forceinline__ int64_t query_row(const QuantAttnParams &p, int b, in
     return (int64_t)b * p.Hq + t * p.heads + hk * g + gg;
 }
 
-// 8 codes (two words, or byte i of eight words) as a bf16 operand.
+// 8 codes (two words) as a bf16 operand.
 template <int F>
 __device__ __forceinline__ uint4 codes_operand(uint32_t lo, uint32_t hi) {
     if constexpr (F == PIKV_QUANT_INT8) {
@@ -68,10 +70,41 @@ __device__ __forceinline__ uint4 codes_operand(uint32_t lo, uint32_t hi) {
     }
 }
 
-template <int W, int F, int QP>
-__global__ __launch_bounds__(kWaves *kWave) void quant_attn_partial(QuantAttnParams p) {
+// Bytes 4 w + 0 .. 3 of four rows, transposed: out[i] holds byte i of each.
+__device__ __forceinline__ void transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t (&out)[4]) {
+    const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), cd0 = __builtin_amdgcn_perm(d, c, 0x05010400u);
+    const uint32_t ab2 = __builtin_amdgcn_perm(b, a, 0x07030602u), cd2 = __builtin_amdgcn_perm(d, c, 0x07030602u);
+    out[0] = __builtin_amdgcn_perm(cd0, ab0, 0x05040100u);
+    out[1] = __builtin_amdgcn_perm(cd0, ab0, 0x07060302u);
+    out[2] = __builtin_amdgcn_perm(cd2, ab2, 0x05040100u);
+    out[3] = __builtin_amdgcn_perm(cd2, ab2, 0x07060302u);
+}
+
+// Loads through a buffer descriptor: a request past its end reads zeros and costs no trip to memory, so that the last tile and
+// the requests ahead of it need no clamps and no branches.  The whole offset goes into the lane's operand, which is what the
+// end is compared with.  (Last operand: non-temporal.)
+template <int BYTES>
+__device__ __forceinline__ void buffer_load(uint32_t (&dst)[BYTES < 4 ? 1 : BYTES / 4], __amdgpu_buffer_rsrc_t rsrc, uint32_t offset) {
+    if constexpr (BYTES == 16) {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, offset, 0, 2);
+        dst[0] = v[0], dst[1] = v[1], dst[2] = v[2], dst[3] = v[3];
+    } else if constexpr (BYTES == 8) {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(rsrc, offset, 0, 2);
+        dst[0] = v[0], dst[1] = v[1];
+    } else if constexpr (BYTES == 4) {
+        dst[0] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, offset, 0, 2);
+    } else {
+        dst[0] = __builtin_amdgcn_raw_buffer_load_b16(rsrc, offset, 0, 2);
+    }
+}
+
+// Blocks a CU holds at the least (registers).
+constexpr int quant_blocks_per_cu(int row_tiles, int parts) { return row_tiles == 1 ? (parts == 1 ? 4 : 3) : row_tiles == 2 ? 2 : 1; }
+
+template <int W, int F, int QP, int RT, bool SC>
+__global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void quant_attn_partial(QuantAttnParams p) {
     constexpr int KB = W / 4 < 16 ? W / 4 : 16, KU = W / 4 / KB;       // bytes of a K piece, pieces of a lane
-    constexpr int KS = W / 32, SETS = W / 16;                           // steps of a score; output sets
+    constexpr int KS = W / 32, SETS = W / 16;                           // steps of a score; output sets, bytes of a V piece
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, r = lane >> 4;
     int split, j, group, row_block;
@@ -80,9 +113,17 @@ __global__ __launch_bounds__(kWaves *kWave) void quant_attn_partial(QuantAttnPar
     const int b = fast_divide(p.by_groups, id, &group);
     const int hk = fast_divide(p.by_row_blocks, group, &row_block);
     const int row0 = row_block * p.rows, rows = min(p.rows, p.G - row0), h0 = hk * p.G + row0;
-    const int e = p.topk[(int64_t)(b * p.rr + (p.rr == 1 ? 0 : h0)) * p.k + j];
+    // One trip to memory: lane e takes shard e's count and addresses beside the selection, which picks among them.
+    const int64_t be_lane = (int64_t)b * p.E + min(lane, p.E - 1);
+    const int n_lane = p.n_valid[be_lane];
+    const uint64_t K_lane = reinterpret_cast<uint64_t>(p.K[be_lane]), V_lane = reinterpret_cast<uint64_t>(p.V[be_lane]);
+    const int e = __builtin_amdgcn_readfirstlane(p.topk[(int64_t)(b * p.rr + (p.rr == 1 ? 0 : h0)) * p.k + j]);
     const int64_t be = (int64_t)b * p.E + e;
-    const int n = min(p.n_valid[be], p.S);
+    const int n = min(__builtin_amdgcn_readlane(n_lane, e), p.S);
+    auto address = [&](uint64_t of_lane) {
+        const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)of_lane, e), hi = __builtin_amdgcn_readlane((int)(uint32_t)(of_lane >> 32), e);
+        return reinterpret_cast<char *>(((uint64_t)hi << 32) | lo) + hk * p.stride_h;
+    };
     int per = p.chunk;
     if (p.nsplit_rcp != 0) {                 // cut by what the shard holds
         constexpr int ROUND = kWaves * kTile;
@@ -100,153 +141,229 @@ __global__ __launch_bounds__(kWaves *kWave) void quant_attn_partial(QuantAttnPar
         }
         return;
     }
-    const char *Kb = static_cast<const char *>(p.K[be]) + hk * p.stride_h, *Vb = static_cast<const char *>(p.V[be]) + hk * p.stride_h;
+    char *Kb = address(K_lane), *Vb = address(V_lane);
+    const uint32_t rb = (uint32_t)p.stride_s;
     const int64_t scale_row = (be * p.Hkv + hk) * p.n_blocks;
+    const float *scales = ((lane & 2) ? p.V_scales : p.K_scales) + scale_row;
 
-    // Query operand of step s = 2 u + v: lane (c, r) holds values 4 KB u + KB r + 8 v + 0 .. 7 of row c.
-    uint4 qop[KS][QP];
-    {
-        const int64_t at = query_row(p, b, hk, row0 + min(c, rows - 1)) * W;
+    // A stage: K rows, V rows and (lanes 0 .. 3: K of either half, V of either) the scales of 32 entries.
+    uint32_t kr[2][KU][KB / 4], vr[8][SETS < 4 ? 1 : SETS / 4];
+    float sr;
+    const uint32_t k_lane = c * rb + KB * r, v_lane = 4 * r * rb + SETS * c;
+    auto opaque = [](uint32_t v) {           // (else an offset per load is carried through the loop)
+        asm volatile("" : "+v"(v));
+        return v;
+    };
+    auto rsrc = [&](char *base, int t0) {    // rows t0 .. of the split: the last one ends after its W bytes
+        const int at = min(t0, last);
+        const uint32_t bytes = at < last ? (uint32_t)(min(last - at, kTile) - 1) * rb + W : 0u;
+        return __builtin_amdgcn_make_buffer_rsrc(base + (int64_t)at * rb, 0, bytes, 0x00020000);
+    };
+    auto load_k = [&](int t0) {
+        sr = scales[min(t0 + 16 * (lane & 1), last - 1) >> p.block_bits];
+        const auto from = rsrc(Kb, t0);
+        const uint32_t at = opaque(k_lane);
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+            for (int u = 0; u < KU; ++u) buffer_load<KB>(kr[hb][u], from, at + 16 * hb * rb + 4 * KB * u);
+    };
+    auto load_v = [&](int t0) {
+        const auto from = rsrc(Vb, t0);
+        const uint32_t at = opaque(v_lane);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) buffer_load<SETS>(vr[t], from, at + (16 * (t >> 2) + (t & 3)) * rb);
+    };
+
+    // Query operand of row tile rt, step s = (KB / 8) u + v: lane (c, r) holds values 4 KB u + KB r + 8 v + 0 .. 7 of its row c.
+    uint4 qop[RT][KS][QP];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int64_t at = query_row(p, b, hk, row0 + min(rt * kRows + c, rows - 1)) * W;
         const bool aligned = (reinterpret_cast<uintptr_t>(p.q) & 15) == 0;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             const int d = 4 * KB * (s / (KB / 8)) + KB * r + 8 * (s % (KB / 8));
             if constexpr (QP == 1) {
-                qop[s][0] = load_query<uint4>(static_cast<const bf16 *>(p.q) + at + d, aligned);
+                qop[rt][s][0] = load_query<uint4>(static_cast<const bf16 *>(p.q) + at + d, aligned);
             } else {
                 float f[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] = static_cast<const float *>(p.q)[at + d + i];
-                split_bf16(f, qop[s]);
+                split_bf16(f, qop[rt][s]);
             }
         }
     }
-
-    float m = -INFINITY, l = 0.0f;
-    f32x4_t acc[SETS];
+    load_k(first + wave * kTile);
+    load_v(first + wave * kTile);
 #pragma unroll
-    for (int i = 0; i < SETS; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int k = 0; k < QP; ++k) hold_operand(qop[rt][s][k]);        // complete here, not behind loads in the loop
+
+    float m[RT], l[RT];
+    f32x4_t acc[RT][SETS];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = -INFINITY;
+        l[rt] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < SETS; ++i) acc[rt][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
 
     for (int t0 = first + wave * kTile; t0 < last; t0 += kWaves * kTile) {
-        float sv[8];
+        // scores sv[rt][4 hb + x]: entry t0 + 16 hb + 4 r + x, row c of row tile rt
+        float sv[RT][8];
+        const int scale_bits = __float_as_int(sr);
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
-            const int slot = min(t0 + 16 * hb + c, last - 1);
-            const char *row = Kb + (int64_t)slot * p.stride_s + KB * r;
-            uint32_t w[KU][KB / 4];
+            const float ks = __int_as_float(__builtin_amdgcn_readlane(scale_bits, hb));
+            f32x4_t sc[RT];
 #pragma unroll
-            for (int u = 0; u < KU; ++u) load_words_stream<KB / 4>(w[u], row + 4 * KB * u);
-            const float ks = p.K_scales[scale_row + (min(t0 + 16 * hb, last - 1) >> p.block_bits)];
-            f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
+            for (int rt = 0; rt < RT; ++rt) sc[rt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = QP - 1; k >= 0; --k)
+            for (int s = 0; s < KS; ++s) {
+                const auto &w = kr[hb][s / (KB / 8)];
+                const int v = s % (KB / 8);
+                const uint4 kop = codes_operand<F>(w[2 * v], w[2 * v + 1]);
 #pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const int u = s / (KB / 8), v = s % (KB / 8);
-                    sc = mfma_rows(codes_operand<F>(w[u][2 * v], w[u][2 * v + 1]), qop[s][k], sc);
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int k = QP - 1; k >= 0; --k) sc[rt] = mfma_rows(kop, qop[rt][s][k], sc[rt]);
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) sv[rt][4 * hb + x] = sc[rt][x] * ks * p.scale;
+        }
+        const float vs0 = __int_as_float(__builtin_amdgcn_readlane(scale_bits, 2)), vs1 = __int_as_float(__builtin_amdgcn_readlane(scale_bits, 3));
+        load_k(t0 + kWaves * kTile);
+        if (t0 + kTile > last) {             // (uniform)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    if (t0 + 16 * (x >> 2) + 4 * r + (x & 3) >= last) sv[rt][x] = -INFINITY;
+        }
+        if constexpr (SC) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                if (rt * kRows + c < rows) {
+                    float *to = p.scores + (((int64_t)b * p.Hq + h0 + rt * kRows + c) * p.k + j) * p.S;
+#pragma unroll
+                    for (int hb = 0; hb < 2; ++hb) {
+                        const int at = t0 + 16 * hb + 4 * r;
+                        if (at + 4 <= last && (p.S & 3) == 0) {
+                            store16(to + at, make_uint4(__float_as_uint(sv[rt][4 * hb]), __float_as_uint(sv[rt][4 * hb + 1]),
+                                                        __float_as_uint(sv[rt][4 * hb + 2]), __float_as_uint(sv[rt][4 * hb + 3])));
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+                                if (at + x < last) to[at + x] = sv[rt][4 * hb + x];
+                        }
+                    }
                 }
+        }
+        uint4 pop[RT][3];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int at = t0 + 16 * hb + 4 * r + x;
-                sv[4 * hb + x] = at < last ? sc[x] * ks * p.scale : -INFINITY;
+        for (int rt = 0; rt < RT; ++rt) {
+            float tm = sv[rt][0];
+#pragma unroll
+            for (int x = 1; x < 8; ++x) tm = fmaxf(tm, sv[rt][x]);
+            const float mn = fmaxf(m[rt], group_max(tm));
+            if (__any(mn > m[rt])) {         // else the factor is 1 in every lane
+                const float corr = __expf(m[rt] - mn);
+                m[rt] = mn;
+                l[rt] *= corr;
+#pragma unroll
+                for (int i = 0; i < SETS; ++i)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) acc[rt][i][x] *= corr;
             }
-            if (p.scores != nullptr && c < rows) {
-                float *to = p.scores + (((int64_t)b * p.Hq + h0 + c) * p.k + j) * p.S + t0 + 16 * hb + 4 * r;
+            float tl[2];
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    if (t0 + 16 * hb + 4 * r + x < last) to[x] = sv[4 * hb + x];
+            for (int hb = 0; hb < 2; ++hb) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) sv[rt][4 * hb + x] = __expf(sv[rt][4 * hb + x] - mn);
+                tl[hb] = (sv[rt][4 * hb] + sv[rt][4 * hb + 1]) + (sv[rt][4 * hb + 2] + sv[rt][4 * hb + 3]);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) sv[rt][4 * hb + x] *= hb ? vs1 : vs0;
+            }
+            l[rt] += tl[0] + tl[1];
+            split_bf16(sv[rt], pop[rt]);
+        }
+        // O^T += V^T P^T, output set i takes byte i of each of the lane's 8 V rows
+        const auto &v = vr;
+#pragma unroll
+        for (int w = 0; w < (SETS + 3) / 4; ++w) {
+            uint32_t lo[4], hi[4];
+            transpose4(v[0][w], v[1][w], v[2][w], v[3][w], lo);
+            transpose4(v[4][w], v[5][w], v[6][w], v[7][w], hi);
+#pragma unroll
+            for (int i = 0; i < (SETS < 4 ? SETS : 4); ++i) {
+                const uint4 vop = codes_operand<F>(lo[i], hi[i]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+                    for (int part = 2; part >= 0; --part) acc[rt][4 * w + i] = mfma_rows(vop, pop[rt][part], acc[rt][4 * w + i]);
+                }
             }
         }
-        float tm = sv[0];
-#pragma unroll
-        for (int x = 1; x < 8; ++x) tm = fmaxf(tm, sv[x]);
-        const float mn = fmaxf(m, group_max(tm)), corr = __expf(m - mn);
-        m = mn;
-        l *= corr;
-#pragma unroll
-        for (int i = 0; i < SETS; ++i)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) acc[i][x] *= corr;
-        float tl = 0.0f;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            sv[x] = __expf(sv[x] - mn);
-            tl += sv[x];
-        }
-        l += tl;
-#pragma unroll
-        for (int hb = 0; hb < 2; ++hb) {
-            const float vs = p.V_scales[scale_row + (min(t0 + 16 * hb, last - 1) >> p.block_bits)];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) sv[4 * hb + x] *= vs;
-        }
-        uint4 pop[3];
-        split_bf16(sv, pop);
-        uint8_t vr[8][SETS];
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            const int slot = min(t0 + 16 * (t >> 2) + 4 * r + (t & 3), last - 1);
-            const char *row = Vb + (int64_t)slot * p.stride_s + SETS * c;
-#pragma unroll
-            for (int i = 0; i < SETS; ++i) vr[t][i] = (uint8_t)row[i];
-        }
-#pragma unroll
-        for (int i = 0; i < SETS; ++i) {
-            uint32_t lo = 0, hi = 0;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                lo |= (uint32_t)vr[t][i] << (8 * t);
-                hi |= (uint32_t)vr[4 + t][i] << (8 * t);
-            }
-            const uint4 vop = codes_operand<F>(lo, hi);
-            f32x4_t small = mfma_rows(vop, pop[2], f32x4_t{0.f, 0.f, 0.f, 0.f});
-            small = mfma_rows(vop, pop[1], small);
-            acc[i] += mfma_rows(vop, pop[0], f32x4_t{0.f, 0.f, 0.f, 0.f}) + small;
-        }
+        load_v(t0 + kWaves * kTile);
     }
 
-    // waves -> LDS -> the block's partial (rows padded by 4 floats: banks)
+    // waves -> LDS -> the block's partial, row tile by row tile (rows padded by 4 floats: banks)
     constexpr int AP = W + 4;
-    __shared__ __attribute__((aligned(16))) float sm_acc[kWaves][kRows][AP];
+    extern __shared__ __attribute__((aligned(16))) float sm_acc[];       // [wave][row][AP], rows of a tile
     __shared__ float sm_m[kWaves][kRows], sm_l[kWaves][kRows];
-    l += __shfl_xor(l, 16, kWave);
-    l += __shfl_xor(l, 32, kWave);
-    if (c < rows) {
+    const int tile_rows = min(kRows, p.rows);
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
+    for (int rt = 0; rt < RT; ++rt) {
+        if (rt * kRows >= rows) break;
+        const int rows_here = min(kRows, rows - rt * kRows);
+        float ls = l[rt];
+        ls += __shfl_xor(ls, 16, kWave);
+        ls += __shfl_xor(ls, 32, kWave);
+        if (rt > 0) __syncthreads();
+        if (c < rows_here) {
 #pragma unroll
-            for (int i = 0; i < SETS; ++i) sm_acc[wave][c][SETS * (4 * r + x) + i] = acc[i][x];
-    }
-    if (r == 0) {
-        sm_m[wave][c] = m;
-        sm_l[wave][c] = l;
-    }
-    __syncthreads();
-    for (int idx = tid; idx < rows * (W / 4); idx += kWaves * kWave) {
-        const int g = idx / (W / 4), d = (idx - g * (W / 4)) * 4;
-        float M = sm_m[0][g];
+            for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm_m[w][g]);
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        float L = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float f = sm_m[w][g] == -INFINITY ? 0.0f : __expf(sm_m[w][g] - M);
-            const float4 o = *reinterpret_cast<const float4 *>(&sm_acc[w][g][d]);
-            a.x = fmaf(o.x, f, a.x);
-            a.y = fmaf(o.y, f, a.y);
-            a.z = fmaf(o.z, f, a.z);
-            a.w = fmaf(o.w, f, a.w);
-            L = fmaf(sm_l[w][g], f, L);
+                for (int i = 0; i < SETS; ++i) sm_acc[(wave * tile_rows + c) * AP + SETS * (4 * r + x) + i] = acc[rt][i][x];
         }
-        const int64_t at = part_base + g * part_row;
-        *reinterpret_cast<float4 *>(p.part_acc + at * W + d) = a;
-        if (d == 0) *reinterpret_cast<float2 *>(p.part_ml + at * 2) = make_float2(M, L);
+        if (r == 0) {
+            sm_m[wave][c] = m[rt];
+            sm_l[wave][c] = ls;
+        }
+        __syncthreads();
+        for (int idx = tid; idx < rows_here * (W / 4); idx += kWaves * kWave) {
+            const int g = idx / (W / 4), d = (idx - g * (W / 4)) * 4;
+            float M = sm_m[0][g];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm_m[w][g]);
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+            float L = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = sm_m[w][g] == -INFINITY ? 0.0f : __expf(sm_m[w][g] - M);
+                const float4 o = *reinterpret_cast<const float4 *>(sm_acc + (w * tile_rows + g) * AP + d);
+                a.x = fmaf(o.x, f, a.x);
+                a.y = fmaf(o.y, f, a.y);
+                a.z = fmaf(o.z, f, a.z);
+                a.w = fmaf(o.w, f, a.w);
+                L = fmaf(sm_l[w][g], f, L);
+            }
+            const int64_t at = part_base + (rt * kRows + g) * part_row;
+            *reinterpret_cast<float4 *>(p.part_acc + at * W + d) = a;
+            if (d == 0) *reinterpret_cast<float2 *>(p.part_ml + at * 2) = make_float2(M, L);
+        }
     }
 }
 
 struct QuantPlan {
-    int rows, row_blocks;      // query rows of a block; row blocks of a kv head
+    int row_tiles, rows, row_blocks;      // matrix tiles and query rows of a block; row blocks of a kv head
     int nsplit, chunk;
     size_t acc_bytes, ml_bytes;
 };
@@ -259,11 +376,15 @@ int make_plan(const pikv_desc *d, int k, QuantPlan *plan) {
     const bool per_head = d->route_rows_per_seq != 1;
     if (tq > 1 && (per_head || d->Hq % tq != 0 || G % tq != 0)) return PIKV_ERR_UNSUPPORTED;
     if (d->stride_s > (1 << 24)) return PIKV_ERR_UNSUPPORTED;
-    plan->rows = per_head ? 1 : G < kRows ? G : kRows;
+    // row tiles of a block: what the group takes, up to four; fp32 queries, three operands each, one
+    plan->row_tiles = per_head || G <= kRows || d->dtype == PIKV_F32 ? 1 : G <= 2 * kRows ? 2 : kMostTiles;
+    plan->rows = per_head ? 1 : G < plan->row_tiles * kRows ? G : plan->row_tiles * kRows;
     plan->row_blocks = (G + plan->rows - 1) / plan->rows;
     const int64_t units = (int64_t)d->B * d->Hkv * plan->row_blocks * k;
-    int64_t nsplit = units > 0 ? 256 * 3 / units : 1;
-    const int64_t most = d->S / (kWaves * kTile);
+    // A block per CU, and blocks of at most 1024 rows, but none of fewer than a stage of each wave.
+    int64_t nsplit = units > 0 ? 256 / units : 1;
+    const int64_t finer = (d->S + kLongestBlock - 1) / kLongestBlock, most = (d->S + kWaves * kTile - 1) / (kWaves * kTile);
+    if (nsplit < finer) nsplit = finer;
     if (nsplit > most) nsplit = most;
     if (nsplit > kMaxPartialsPerHead / k) nsplit = kMaxPartialsPerHead / k;
     if (nsplit < 1) nsplit = 1;
@@ -364,11 +485,20 @@ extern "C" int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t bl
     c.by_G = fast_div(c.G);
     c.decoder_bytes = 0;
     const dim3 grid((unsigned)((int64_t)desc->B * desc->Hkv * plan.row_blocks * k * plan.nsplit)), threads(kWaves * kWave);
+    const size_t lds = (size_t)kWaves * (plan.rows < kRows ? plan.rows : kRows) * (desc->D + 4) * sizeof(float);
     hipStream_t st = as_stream(stream);
     auto launch = [&](auto width, auto fmt) {
         constexpr int W = decltype(width)::value, F = decltype(fmt)::value;
-        if (desc->dtype == PIKV_F32) hipLaunchKernelGGL((quant_attn_partial<W, F, 3>), grid, threads, 0, st, p);
-        else hipLaunchKernelGGL((quant_attn_partial<W, F, 1>), grid, threads, 0, st, p);
+        auto go = [&](auto parts, auto tiles) {
+            constexpr int QP = decltype(parts)::value, RT = decltype(tiles)::value;
+            if (scores) hipLaunchKernelGGL((quant_attn_partial<W, F, QP, RT, true>), grid, threads, lds, st, p);
+            else hipLaunchKernelGGL((quant_attn_partial<W, F, QP, RT, false>), grid, threads, lds, st, p);
+        };
+        const std::integral_constant<int, 1> one{};
+        if (desc->dtype == PIKV_F32) go(std::integral_constant<int, 3>{}, one);
+        else if (plan.row_tiles == 1) go(one, one);
+        else if (plan.row_tiles == 2) go(one, std::integral_constant<int, 2>{});
+        else go(one, std::integral_constant<int, kMostTiles>{});
     };
     auto by_width = [&](auto fmt) {
         if (desc->D == 32) launch(std::integral_constant<int, 32>{}, fmt);

@@ -16,7 +16,7 @@ inline int check_quant(const pikv_desc *d, int format, int block) {
     if (rc != PIKV_OK) return rc;
     if (format != PIKV_QUANT_INT8 && format != PIKV_QUANT_E4M3) return PIKV_ERR_INVALID;
     if (block != 16 && block != 32 && block != 64 && block != 128) return PIKV_ERR_INVALID;
-    if (d->rank != 0 || d->D < 32) return PIKV_ERR_UNSUPPORTED;
+    if (d->rank != 0 || d->D < 32 || d->S > (1 << 30)) return PIKV_ERR_UNSUPPORTED;
     if (d->stride_s % 16 != 0 || d->stride_h % 16 != 0) return PIKV_ERR_INVALID;     // bytes
     return PIKV_OK;
 }
