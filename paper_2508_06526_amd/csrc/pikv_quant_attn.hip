@@ -27,7 +27,9 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kRows = 16;               // query rows of a matrix tile
 constexpr int kTile = 32;               // entries of a stage of a wave
-constexpr int kMostTiles = 4;           // row tiles of a block
+// Row tiles of a block, at most.  (Four fit a CU once, with their accumulators moved to and fro: 64 rows over 128 MiB's worth of
+// 32K entries 26.5 us, as two blocks of two, the second reading from the caches, 22.7, as four of one 25.9; 32 rows: 23.7, 28.7.)
+constexpr int kMostTiles = 2;
 constexpr int kLongestBlock = 1024;     // rows of a block, while the merge holds the partials
 
 struct QuantAttnParams {
@@ -99,7 +101,7 @@ __device__ __forceinline__ void buffer_load(uint32_t (&dst)[BYTES < 4 ? 1 : BYTE
 }
 
 // Blocks a CU holds at the least (registers).
-constexpr int quant_blocks_per_cu(int row_tiles, int parts) { return row_tiles == 1 ? (parts == 1 ? 4 : 3) : row_tiles == 2 ? 2 : 1; }
+constexpr int quant_blocks_per_cu(int row_tiles, int parts) { return row_tiles == 1 ? (parts == 1 ? 4 : 3) : 2; }
 
 template <int W, int F, int QP, int RT, bool SC>
 __global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void quant_attn_partial(QuantAttnParams p) {
@@ -376,8 +378,8 @@ int make_plan(const pikv_desc *d, int k, QuantPlan *plan) {
     const bool per_head = d->route_rows_per_seq != 1;
     if (tq > 1 && (per_head || d->Hq % tq != 0 || G % tq != 0)) return PIKV_ERR_UNSUPPORTED;
     if (d->stride_s > (1 << 24)) return PIKV_ERR_UNSUPPORTED;
-    // row tiles of a block: what the group takes, up to four; fp32 queries, three operands each, one
-    plan->row_tiles = per_head || G <= kRows || d->dtype == PIKV_F32 ? 1 : G <= 2 * kRows ? 2 : kMostTiles;
+    // row tiles of a block: what the group takes; fp32 queries, three operands each, one
+    plan->row_tiles = per_head || G <= kRows || d->dtype == PIKV_F32 ? 1 : kMostTiles;
     plan->rows = per_head ? 1 : G < plan->row_tiles * kRows ? G : plan->row_tiles * kRows;
     plan->row_blocks = (G + plan->rows - 1) / plan->rows;
     const int64_t units = (int64_t)d->B * d->Hkv * plan->row_blocks * k;
@@ -497,7 +499,6 @@ extern "C" int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t bl
         const std::integral_constant<int, 1> one{};
         if (desc->dtype == PIKV_F32) go(std::integral_constant<int, 3>{}, one);
         else if (plan.row_tiles == 1) go(one, one);
-        else if (plan.row_tiles == 2) go(one, std::integral_constant<int, 2>{});
         else go(one, std::integral_constant<int, kMostTiles>{});
     };
     auto by_width = [&](auto fmt) {
