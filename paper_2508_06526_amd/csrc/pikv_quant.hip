@@ -5,6 +5,10 @@
 //                  then the largest), joins it with the waves of the same scale block and writes codes and scale: one pass
 //                  over the dense rows.
 //   quant_read   : the same tiles the other way, value = code * scale.
+//   Both are bound by memory.  Dense rows, read or written once, go past the caches (non-temporal), codes, which the next call
+//   reads, do not: written and read back, 2.7 GB in fp32 in 396 us (6.8 TB/s; all through the caches 495, codes past them too 425 -
+//   448), 1.6 GB in bf16 in 236 us (292; 237 - 257).  16-byte pieces of neighbouring lanes: with 8 fp32 values
+//   a lane, two pieces, half of every line was written at a time (127 MB 38 -> 26.7 us).
 //   quant_append : one block per (sequence, selected expert): slot rule and count of append_rows; a row of D values by D / 8
 //                  lanes, which also round the codes of the block's other live slots where its scale grows.
 #include "pikv_mfma_dev.h"
@@ -30,21 +34,11 @@ struct Eight {
         for (int i = 0; i < N; ++i) Pack16<T>::widen(v[i], f + i * Pack16<T>::N);
     }
 };
-template <typename T>
-__device__ __forceinline__ void store8(T *p, const float *f) {
-    if constexpr (sizeof(T) == 4) {
-        store16(p, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
-        store16(p + 4, make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])));
-    } else {
-        uint4 out[1];
-        split_bf16(f, out);
-        store16(p, out[0]);
-    }
-}
-__device__ __forceinline__ uint32_t magnitude(const float *f) {
+template <int N>
+__device__ __forceinline__ uint32_t magnitude(const float (&f)[N]) {
     uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(f[i]) & 0x7fffffffu);
+    for (int i = 0; i < N; ++i) most = max(most, __float_as_uint(f[i]) & 0x7fffffffu);
     return most;
 }
 // The largest of COUNT (a power of two) adjacent lanes' values, in all of them.
@@ -79,25 +73,26 @@ __device__ __forceinline__ bool find_tile(const QuantParams &p, int slots, Tile 
     return t->first < t->n;
 }
 
+// A lane's values are one 16-byte load: 8 of bf16, 4 of fp32.
 template <typename T, int D, int F, int WAVES>
 __global__ __launch_bounds__(WAVES *kWave) void quant_pack(QuantParams p) {
-    constexpr int LPR = D / 8, RPL = kWave / LPR, NL = kWaveSlots / RPL;     // lanes of a row, rows of a load, loads
+    constexpr int VPL = Pack16<T>::N, LPR = D / VPL, RPL = kWave / LPR, NL = kWaveSlots / RPL;     // values of a lane, lanes of a row, rows of a load, loads
     __shared__ uint32_t wave_most[WAVES];
     Tile t;
     if (!find_tile(p, WAVES * kWaveSlots, &t)) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
     const int c = lane & (LPR - 1), r = lane / LPR;
     const int s0 = t.first + wave * kWaveSlots;
-    const T *rows = static_cast<const T *>(t.v ? p.V_dense[t.be] : p.K_dense[t.be]) + t.h * p.dense_h + 8 * c;
-    char *codes = static_cast<char *>(t.v ? p.V[t.be] : p.K[t.be]) + t.h * p.code_h + 8 * c;
-    Eight<T> x[NL];
+    const T *rows = static_cast<const T *>(t.v ? p.V_dense[t.be] : p.K_dense[t.be]) + t.h * p.dense_h + VPL * c;
+    char *codes = static_cast<char *>(t.v ? p.V[t.be] : p.K[t.be]) + t.h * p.code_h + VPL * c;
+    uint4 x[NL];
 #pragma unroll
-    for (int i = 0; i < NL; ++i) x[i].load(rows + (int64_t)min(s0 + i * RPL + r, t.n - 1) * p.dense_s);    // (past the end: the last valid row)
+    for (int i = 0; i < NL; ++i) x[i] = load16_stream(rows + (int64_t)min(s0 + i * RPL + r, t.n - 1) * p.dense_s);    // (past the end: the last valid row)
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-        float f[8];
-        x[i].widen(f);
+        float f[VPL];
+        Pack16<T>::widen(x[i], f);
         if (s0 + i * RPL + r < t.n) most = max(most, magnitude(f));
     }
     most = lanes_max<kWave>(most);
@@ -114,38 +109,48 @@ __global__ __launch_bounds__(WAVES *kWave) void quant_pack(QuantParams p) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
         const int slot = s0 + i * RPL + r;
-        float f[8];
-        x[i].widen(f);
-        const uint2 w = make_uint2(encode4<F>(f, inv), encode4<F>(f + 4, inv));
-        if (slot < t.n) *reinterpret_cast<uint2 *>(codes + (int64_t)slot * p.code_s) = w;
+        float f[VPL];
+        Pack16<T>::widen(x[i], f);
+        uint32_t w[VPL / 4];
+#pragma unroll
+        for (int u = 0; u < VPL / 4; ++u) w[u] = encode4<F>(f + 4 * u, inv);
+        char *to = codes + (int64_t)slot * p.code_s;
+        if (slot < t.n) {
+            if constexpr (VPL == 4) *reinterpret_cast<uint32_t *>(to) = w[0];
+            else *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+        }
     }
 }
 
 template <typename T, int D, int F>
 __global__ __launch_bounds__(256) void quant_read(QuantParams p) {
-    constexpr int LPR = D / 8, RPL = kWave / LPR, NL = kWaveSlots / RPL;
+    constexpr int VPL = Pack16<T>::N, LPR = D / VPL, RPL = kWave / LPR, NL = kWaveSlots / RPL;
     Tile t;
     if (!find_tile(p, kTileSlots, &t)) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
     const int c = lane & (LPR - 1), r = lane / LPR;
     const int s0 = t.first + wave * kWaveSlots;
     if (s0 >= t.n) return;
-    T *rows = static_cast<T *>(const_cast<void *>(t.v ? p.V_dense[t.be] : p.K_dense[t.be])) + t.h * p.dense_h + 8 * c;
-    const char *codes = static_cast<const char *>(t.v ? p.V[t.be] : p.K[t.be]) + t.h * p.code_h + 8 * c;
+    T *rows = static_cast<T *>(const_cast<void *>(t.v ? p.V_dense[t.be] : p.K_dense[t.be])) + t.h * p.dense_h + VPL * c;
+    const char *codes = static_cast<const char *>(t.v ? p.V[t.be] : p.K[t.be]) + t.h * p.code_h + VPL * c;
     const float scale = (t.v ? p.V_scales : p.K_scales)[((int64_t)t.be * p.Hkv + t.h) * p.n_blocks + (s0 >> p.block_bits)];
-    uint2 w[NL];
+    typedef uint32_t Codes __attribute__((ext_vector_type(VPL / 4)));
+    Codes w[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i)
-        w[i] = *reinterpret_cast<const uint2 *>(codes + (int64_t)min(s0 + i * RPL + r, t.n - 1) * p.code_s);
+        w[i] = *reinterpret_cast<const Codes *>(codes + (int64_t)min(s0 + i * RPL + r, t.n - 1) * p.code_s);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
         const int slot = s0 + i * RPL + r;
-        float f[8];
-        decode4<F>(w[i].x, f);
-        decode4<F>(w[i].y, f + 4);
+        float f[VPL];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) f[u] *= scale;
-        if (slot < t.n) store8(rows + (int64_t)slot * p.dense_s, f);
+        for (int u = 0; u < VPL / 4; ++u) decode4<F>(w[i][u], f + 4 * u);
+#pragma unroll
+        for (int u = 0; u < VPL; ++u) f[u] *= scale;
+        uint4 out[1];
+        if constexpr (VPL == 4) out[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+        else split_bf16(f, out);
+        if (slot < t.n) store16_stream(rows + (int64_t)slot * p.dense_s, out[0]);
     }
 }
 
@@ -160,47 +165,72 @@ struct QuantAppendParams {
     int E, S, Hkv, k, max_evict, n_blocks, block_bits;
 };
 
+// Two trips to memory, as append_rows: lane e takes shard e's count, freed slot and addresses beside the selection, which picks
+// among them, and the new rows come with those; then the block's old scale - and, where it grows, a third for its codes, eight
+// slots at a time.
 template <typename T, int D, int F>
 __global__ __launch_bounds__(1024) void quant_append(QuantAppendParams p) {
     constexpr int LPR = D / 8;
     int j;
     const int b = fast_divide(p.by_k, blockIdx.x, &j);
-    const int tid = threadIdx.x, c = tid & (LPR - 1);
-    const int e = p.topk[(int64_t)b * p.k + j];
-    const int64_t be = (int64_t)b * p.E + e;
-    const int n = p.n_valid[be];
-    const int cnt = p.reuse_cnt ? p.reuse_cnt[be] : 0;
-    const int slot = cnt > 0 ? p.reuse_idx[be * p.max_evict] : n;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), c = tid & (LPR - 1);
+    const int64_t be0 = (int64_t)b * p.E, be_lane = be0 + min(lane, p.E - 1);
+    const int sel = p.topk[(int64_t)b * p.k + min(lane, p.k - 1)];
+    const int n_lane = p.n_valid[be_lane];
+    const uint64_t K_lane = reinterpret_cast<uint64_t>(p.K[be_lane]), V_lane = reinterpret_cast<uint64_t>(p.V[be_lane]);
+    int cnt_lane = 0, idx_lane = 0;
+    if (p.reuse_cnt) {                       // block-uniform
+        cnt_lane = p.reuse_cnt[be_lane];
+        idx_lane = p.reuse_idx[be_lane * p.max_evict];
+    }
+    const int row_step = blockDim.x / LPR, rows = 2 * p.Hkv;           // a row: (kv head, K or V), by D / 8 lanes of one wave
+    auto new_row = [&](int row) {
+        Eight<T> x;
+        x.load(static_cast<const T *>((row & 1) ? p.V_new : p.K_new) + ((int64_t)b * p.Hkv + (row >> 1)) * D + 8 * c);
+        return x;
+    };
+    Eight<T> x = new_row(min(tid / LPR, rows - 1));
+    const int e = __builtin_amdgcn_readlane(sel, j), n = __builtin_amdgcn_readlane(n_lane, e), cnt = __builtin_amdgcn_readlane(cnt_lane, e);
+    const int slot = cnt > 0 ? __builtin_amdgcn_readlane(idx_lane, e) : n;
     __syncthreads();                         // every thread has read n before it changes
     if (n >= p.S || slot < 0 || slot >= p.S) return;   // full shard: the entry is dropped
+    const int64_t be = be0 + e;
     const int blk = slot >> p.block_bits, lo = blk << p.block_bits;
     const int live = min(p.S, n + max(cnt, 1)), hi = min(lo + (1 << p.block_bits), live);      // live slots of the block: lo .. hi - 1
     const bool others = hi - lo > (slot < hi ? 1 : 0);
-    const int row_step = blockDim.x / LPR;
-    for (int row = tid / LPR; row < 2 * p.Hkv; row += row_step) {      // (kv head, K or V); D / 8 lanes of one wave
+    auto address = [&](uint64_t of_lane) {
+        const uint32_t low = __builtin_amdgcn_readlane((int)(uint32_t)of_lane, e), high = __builtin_amdgcn_readlane((int)(uint32_t)(of_lane >> 32), e);
+        return reinterpret_cast<char *>(((uint64_t)high << 32) | low);
+    };
+    char *Ks = address(K_lane), *Vs = address(V_lane);
+    for (int row = tid / LPR; row < rows; row += row_step) {
         const int h = row >> 1, v = row & 1;
-        Eight<T> x;
-        x.load(static_cast<const T *>(v ? p.V_new : p.K_new) + ((int64_t)b * p.Hkv + h) * D + 8 * c);
+        if (row >= row_step) x = new_row(row);
         float *at = (v ? p.V_scales : p.K_scales) + (be * p.Hkv + h) * p.n_blocks + blk;
-        const uint32_t old = __float_as_uint(*at);
-        char *codes = static_cast<char *>(v ? p.V[be] : p.K[be]) + h * p.code_h + 8 * c;
+        const uint32_t old = __float_as_uint(*at) & 0x7fffffffu;
+        char *codes = (v ? Vs : Ks) + h * p.code_h + 8 * c;
         float f[8];
         x.widen(f);
         uint32_t scale = needed_scale<F>(lanes_max<LPR>(magnitude(f)));
-        if (others) scale = max(scale, old & 0x7fffffffu);
+        if (others) scale = max(scale, old);
         const float inv = inverse_scale(scale);
-        if (others && scale != (old & 0x7fffffffu)) {
+        if (others && scale != old) {
             // old / scale, at most 1/2; 0 from where it underflows, and codes with it (NaN scale: 0)
             const int shift = (int)(scale >> 23) - (int)(old >> 23);
             const float ratio = scale >= 0x7f800000u || shift > 126 ? 0.0f : __uint_as_float((uint32_t)(127 - shift) << 23);
-            for (int s = lo; s < hi; ++s) {
-                if (s == slot) continue;
-                uint2 *held = reinterpret_cast<uint2 *>(codes + (int64_t)s * p.code_s);
-                const uint2 w = *held;
-                float g[8];
-                decode4<F>(w.x, g);
-                decode4<F>(w.y, g + 4);
-                *held = make_uint2(encode4<F>(g, ratio), encode4<F>(g + 4, ratio));
+            constexpr int kAtOnce = 8;
+            for (int s0 = lo; s0 < hi; s0 += kAtOnce) {
+                uint2 w[kAtOnce];
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) w[u] = *reinterpret_cast<const uint2 *>(codes + (int64_t)min(s0 + u, hi - 1) * p.code_s);
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) {
+                    float g[8];
+                    decode4<F>(w[u].x, g);
+                    decode4<F>(w[u].y, g + 4);
+                    const uint2 to = make_uint2(encode4<F>(g, ratio), encode4<F>(g + 4, ratio));
+                    if (s0 + u < hi && s0 + u != slot) *reinterpret_cast<uint2 *>(codes + (int64_t)(s0 + u) * p.code_s) = to;
+                }
             }
         }
         *reinterpret_cast<uint2 *>(codes + (int64_t)slot * p.code_s) = make_uint2(encode4<F>(f, inv), encode4<F>(f + 4, inv));

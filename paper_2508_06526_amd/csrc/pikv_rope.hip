@@ -1,9 +1,13 @@
 // Norms of queries and keys for each head and the position rotation, out of a fused projection.
 //
-//   norm_rope : a block takes heads of one token, D / 8 lanes a head, 8 values a lane (loaded and stored in 16-byte pieces).
+//   norm_rope : a block takes heads of one token, a 16-byte piece of a head per lane.
 //               The sum of squares is joined by a butterfly over the head's lanes; the partner of a value in the rotation sits
-//               rotary_dim / 16 lanes away (or in the same lane, interleaved).  The angles of a token are the same for all of its
+//               rotary_dim / 2 values, whole lanes, away (or in the same lane, interleaved).  The angles of a token are the same for all of its
 //               heads: cosines and sines are formed once per block, behind the first request for rows, and kept in LDS.
+//
+// Bound by memory, 16384 tokens x 48 heads of 128 bf16 values in 58.9 us (6.84 TB/s), a token in 2.4 us of the GPU's time: the
+// launch and two trips to memory.  Rows come through the caches, where the projection has left them, outputs go past (with
+// ordinary stores 75 us, with rows past the caches as well 70).
 //
 // Angle = position * inv_freq: in fp32 the product of a far position is off by its own rounding (position 10^6: 0.03
 // radians), so it is formed in 64 bits, in revolutions, and only what is left after whole ones is rounded.
@@ -29,76 +33,69 @@ constexpr int kRopeThreads = 256;
 
 template <typename T, int D>
 __global__ __launch_bounds__(kRopeThreads) void norm_rope(RopeParams p) {
-    constexpr int LPR = D / 8, STEP = kRopeThreads / LPR, N = sizeof(T) / 2;      // lanes of a head, heads at once, 16-byte pieces of 8 values
+    constexpr int VPL = Pack16<T>::N, LPR = D / VPL, STEP = kRopeThreads / LPR;      // values of a lane, lanes of a head, heads at once
     __shared__ float cos_s[64], sin_s[64];
     int part;
     const int token = fast_divide(p.by_parts, blockIdx.x, &part);
     const int tid = threadIdx.x, c = tid & (LPR - 1);
-    const int last = min(p.heads, (part + 1) * p.per_block);
+    const int first = part * p.per_block + tid / LPR, last = min(p.heads, (part + 1) * p.per_block);
     const int half = p.rotary >> 1;
+    const T *row = static_cast<const T *>(p.x) + token * p.token_stride + VPL * c;
+    auto load = [&](int head) { return load16(row + (int64_t)min(head, last - 1) * D); };      // (past the end: the last head once more)
+    uint4 next = load(first);                // ahead of the angles
     if (tid < half) {
         const double turns = (double)p.positions[token] * (double)p.inv_freq[tid] * 0.15915494309189533577;      // 1 / (2 pi)
         sincospif((float)(2.0 * (turns - rint(turns))), &sin_s[tid], &cos_s[tid]);
     }
     __syncthreads();
-    const T *row = static_cast<const T *>(p.x) + token * p.token_stride;
-    for (int head = part * p.per_block + tid / LPR; head < last; head += STEP) {
-        uint4 raw[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) raw[i] = load16(reinterpret_cast<const char *>(row + (int64_t)head * D + 8 * c) + 16 * i);
+    for (int head = first; head < last; head += STEP) {
+        const uint4 raw = next;
+        if (head + STEP < last) next = load(head + STEP);
         const bool key = head >= p.Hq && head < p.Hq + p.Hkv, value = head >= p.Hq + p.Hkv;
         T *out;
         if (value) out = static_cast<T *>(p.v_out) + ((int64_t)token * p.Hkv + head - p.Hq - p.Hkv) * D;
         else if (key) out = static_cast<T *>(p.k_out) + ((int64_t)token * p.Hkv + head - p.Hq) * D;
         else out = static_cast<T *>(p.q_out) + ((int64_t)token * p.Hq + head) * D;
-        out += 8 * c;
+        out += VPL * c;
         if (value) {                                  // copied as they are
-#pragma unroll
-            for (int i = 0; i < N; ++i) store16(reinterpret_cast<char *>(out) + 16 * i, raw[i]);
+            store16_stream(out, raw);
             continue;
         }
-        float z[8];
-#pragma unroll
-        for (int i = 0; i < N; ++i) Pack16<T>::widen(raw[i], z + i * Pack16<T>::N);
+        float z[VPL];
+        Pack16<T>::widen(raw, z);
         const T *w = static_cast<const T *>(key ? p.w_k : p.w_q);
         if (w != nullptr) {
             float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(z[i], z[i], sum);
+            for (int i = 0; i < VPL; ++i) sum = fmaf(z[i], z[i], sum);
 #pragma unroll
             for (int off = 1; off < LPR; off <<= 1) sum += __shfl_xor(sum, off, kWave);
             const float r = 1.0f / sqrtf(sum * (1.0f / D) + p.eps);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = z[i] * r * load_scalar<T>(w, 8 * c + i);
+            for (int i = 0; i < VPL; ++i) z[i] = z[i] * r * load_scalar<T>(w, VPL * c + i);
         }
-        if (8 * c < p.rotary) {                       // (rotary: a multiple of 16; a head's rotated lanes are whole pairs)
+        if (VPL * c < p.rotary) {                       // (rotary: a multiple of 16; a head's rotated lanes are whole pairs)
             if (p.interleaved) {
 #pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    const float cs = cos_s[4 * c + i / 2], sn = sin_s[4 * c + i / 2], a = z[i], b = z[i + 1];
+                for (int i = 0; i < VPL; i += 2) {
+                    const float cs = cos_s[(VPL * c + i) / 2], sn = sin_s[(VPL * c + i) / 2], a = z[i], b = z[i + 1];
                     z[i] = a * cs - b * sn;
                     z[i + 1] = b * cs + a * sn;
                 }
             } else {
-                const bool second = 8 * c >= half;
-                const int lane = tid & (kWave - 1), other = second ? lane - half / 8 : lane + half / 8, i0 = second ? 8 * c - half : 8 * c;
+                const bool second = VPL * c >= half;
+                const int lane = tid & (kWave - 1), other = second ? lane - half / VPL : lane + half / VPL, i0 = second ? VPL * c - half : VPL * c;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < VPL; ++i) {
                     const float with = __shfl(z[i], other, kWave), cs = cos_s[i0 + i], sn = sin_s[i0 + i];
                     z[i] = second ? z[i] * cs + with * sn : z[i] * cs - with * sn;
                 }
             }
         }
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                store16(out + 4 * i, make_uint4(__float_as_uint(z[4 * i]), __float_as_uint(z[4 * i + 1]), __float_as_uint(z[4 * i + 2]),
-                                                __float_as_uint(z[4 * i + 3])));
-        } else {
-            uint4 packed[1];
-            split_bf16(z, packed);
-            store16(out, packed[0]);
-        }
+        uint4 packed[1];
+        if constexpr (VPL == 4) packed[0] = make_uint4(__float_as_uint(z[0]), __float_as_uint(z[1]), __float_as_uint(z[2]), __float_as_uint(z[3]));
+        else split_bf16(z, packed);
+        store16_stream(out, packed[0]);
     }
 }
 
@@ -139,9 +136,11 @@ extern "C" int pikv_norm_rope(const void *x, int32_t tokens, int64_t token_strid
     p.interleaved = interleaved ? 1 : 0;
     p.eps = eps;
     p.heads = (int)heads;
-    const int at_once = kRopeThreads / (D / 8), passes = (p.heads + at_once - 1) / at_once;
-    const int parts = passes;
-    p.per_block = at_once;
+    const int at_once = kRopeThreads * 16 / (D * elem_bytes(dtype)), passes = (p.heads + at_once - 1) / at_once;
+    // Few tokens: a block for each pass over heads, so that the passes run side by side (512 tokens x 80 heads of 128 values 6.7 against
+    // 8.3 us).  Many: one block for all of a token's heads, its angles formed once (4096 tokens 36.7 -> 30.4).
+    const int parts = (int64_t)tokens * passes <= 4096 ? passes : 1;
+    p.per_block = parts > 1 ? at_once : p.heads;
     p.by_parts = fast_div(parts);
     if ((int64_t)tokens * parts > (1 << 23)) return PIKV_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)(tokens * parts));
