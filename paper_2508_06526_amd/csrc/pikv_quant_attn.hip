@@ -26,6 +26,7 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kRows = 16;               // query rows of a matrix tile
+constexpr int kMergedWaves = 8;         // of a block that takes all shards of its rows
 constexpr int kTile = 32;               // entries of a stage of a wave
 // Row tiles of a block, at most.  (Four fit a CU once, with their accumulators moved to and fro: 64 rows over 128 MiB's worth of
 // 32K entries 26.5 us, as two blocks of two, the second reading from the caches, 22.7, as four of one 25.9; 32 rows: 23.7, 28.7.)
@@ -44,6 +45,12 @@ struct QuantAttnParams {
     int nsplit, chunk, n_blocks, block_bits;
     uint32_t nsplit_rcp;
     float scale;
+    int shard_waves;                   // merged form: waves of a shard
+    struct {
+        const float *gates;
+        float *y, *row_max, *row_norm, *slot_coef;
+        int combine;
+    } merge;
 };
 
 // Where the caller keeps query row `row` of kv head hk (rows of a kv head: draft query, head of the group).
@@ -84,34 +91,76 @@ __device__ __forceinline__ void transpose4(uint32_t a, uint32_t b, uint32_t c, u
 
 // Loads through a buffer descriptor: a request past its end reads zeros and costs no trip to memory, so that the last tile and
 // the requests ahead of it need no clamps and no branches.  The whole offset goes into the lane's operand, which is what the
-// end is compared with.  (Last operand: non-temporal.)
-template <int BYTES>
+// end is compared with.  NT: non-temporal, for what no later request finds part of in the caches.
+template <int BYTES, bool NT>
 __device__ __forceinline__ void buffer_load(uint32_t (&dst)[BYTES < 4 ? 1 : BYTES / 4], __amdgpu_buffer_rsrc_t rsrc, uint32_t offset) {
     if constexpr (BYTES == 16) {
-        const auto v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, offset, 0, 2);
+        const auto v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, offset, 0, NT ? 2 : 0);
         dst[0] = v[0], dst[1] = v[1], dst[2] = v[2], dst[3] = v[3];
     } else if constexpr (BYTES == 8) {
-        const auto v = __builtin_amdgcn_raw_buffer_load_b64(rsrc, offset, 0, 2);
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(rsrc, offset, 0, NT ? 2 : 0);
         dst[0] = v[0], dst[1] = v[1];
     } else if constexpr (BYTES == 4) {
-        dst[0] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, offset, 0, 2);
+        dst[0] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, offset, 0, NT ? 2 : 0);
     } else {
-        dst[0] = __builtin_amdgcn_raw_buffer_load_b16(rsrc, offset, 0, 2);
+        dst[0] = __builtin_amdgcn_raw_buffer_load_b16(rsrc, offset, 0, NT ? 2 : 0);
     }
 }
 
 // Blocks a CU holds at the least (registers).
 constexpr int quant_blocks_per_cu(int row_tiles, int parts) { return row_tiles == 1 ? (parts == 1 ? 4 : 3) : 2; }
 
-template <int W, int F, int QP, int RT, bool SC>
-__global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void quant_attn_partial(QuantAttnParams p) {
+// The merge of a block that holds all selected shards of its rows: 8 lanes a row, lane w with wave w's (max, sum) pair.  A
+// shard's waves are 8, 4, 2 or 1 neighbours: joined by an xor butterfly, then the shards with their gates (as head_weights, in
+// both combine modes).  Leaves every wave's factor.
+__device__ __forceinline__ void merge_rows(const QuantAttnParams &p, int b, int h0, int hk, int row0, int rows, float gate, const float (&m)[kMergedWaves][kRows],
+                                           const float (&l)[kMergedWaves][kRows], float (&factor)[kMergedWaves][kRows]) {
+    static_assert(kMergedWaves == 8, "a row is 8 lanes");
+    const int g = threadIdx.x >> 3, w = threadIdx.x & 7, per = p.shard_waves, j = w / per;
+    if (threadIdx.x >= kRows * 8) return;    // whole waves
+    const bool used = g < rows && j < p.k;
+    const float mw = used ? m[w][g] : -INFINITY, lw = used ? l[w][g] : 0.0f;
+    float Mj = mw;
+    for (int off = 1; off < per; off <<= 1) Mj = fmaxf(Mj, __shfl_xor(Mj, off, kWave));
+    float Zj = mw == -INFINITY ? lw : lw * __expf(mw - Mj);                    // (a wave without rows: 0)
+    for (int off = 1; off < per; off <<= 1) Zj += __shfl_xor(Zj, off, kWave);
+    const bool live = Zj > 0.0f, lse = p.merge.combine == PIKV_COMBINE_LSE;
+    float M = live ? Mj : -INFINITY;
+    for (int off = per; off < 8; off <<= 1) M = fmaxf(M, __shfl_xor(M, off, kWave));
+    const float e = __expf(Mj - M);
+    float norm = live ? (lse ? gate * Zj * e : gate) : 0.0f;
+    for (int off = per; off < 8; off <<= 1) norm += __shfl_xor(norm, off, kWave);
+    if (!used) return;
+    const float weight = !live ? 0.0f : lse ? gate * e / norm : gate / (norm * Zj);
+    factor[w][g] = lw > 0.0f && live ? weight * __expf(mw - Mj) : 0.0f;
+    if (w % per == 0 && p.merge.slot_coef) {
+        float *to = p.merge.slot_coef + (((int64_t)b * p.Hq + h0 + g) * p.k + j) * 2;
+        to[0] = !live ? 0.0f : lse ? M : Mj;
+        to[1] = !live ? 0.0f : lse ? gate / norm : weight;
+    }
+    if (w == 0) {
+        const int64_t row = query_row(p, b, hk, row0 + g);
+        if (p.merge.row_max) p.merge.row_max[row] = M;
+        if (p.merge.row_norm) p.merge.row_norm[row] = norm;
+    }
+}
+
+// WAVES == kWaves: a split of a shard, partials for the merge.  WAVES == kMergedWaves: all selected shards of the rows by one
+// block, some of its waves each, and the merge behind them: short calls in one launch.
+template <int W, int F, int QP, int RT, bool SC, int WAVES>
+__global__ __launch_bounds__(WAVES *kWave, WAVES == kWaves ? quant_blocks_per_cu(RT, QP) : 1) void quant_attn_partial(QuantAttnParams p) {
+    constexpr bool MERGED = WAVES == kMergedWaves;
     constexpr int KB = W / 4 < 16 ? W / 4 : 16, KU = W / 4 / KB;       // bytes of a K piece, pieces of a lane
     constexpr int KS = W / 32, SETS = W / 16;                           // steps of a score; output sets, bytes of a V piece
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, r = lane >> 4;
-    int split, j, group, row_block;
-    int id = fast_divide(p.by_nsplit, blockIdx.x, &split);
-    id = fast_divide(p.by_k, id, &j);
+    int split = 0, j, group, row_block, id = blockIdx.x;
+    if constexpr (MERGED) {
+        j = min(wave / p.shard_waves, p.k);              // (k: a wave that is left over)
+    } else {
+        id = fast_divide(p.by_nsplit, id, &split);
+        id = fast_divide(p.by_k, id, &j);
+    }
     const int b = fast_divide(p.by_groups, id, &group);
     const int hk = fast_divide(p.by_row_blocks, group, &row_block);
     const int row0 = row_block * p.rows, rows = min(p.rows, p.G - row0), h0 = hk * p.G + row0;
@@ -119,7 +168,9 @@ __global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void qu
     const int64_t be_lane = (int64_t)b * p.E + min(lane, p.E - 1);
     const int n_lane = p.n_valid[be_lane];
     const uint64_t K_lane = reinterpret_cast<uint64_t>(p.K[be_lane]), V_lane = reinterpret_cast<uint64_t>(p.V[be_lane]);
-    const int e = __builtin_amdgcn_readfirstlane(p.topk[(int64_t)(b * p.rr + (p.rr == 1 ? 0 : h0)) * p.k + j]);
+    const int e = __builtin_amdgcn_readfirstlane(p.topk[(int64_t)(b * p.rr + (p.rr == 1 ? 0 : h0)) * p.k + min(j, p.k - 1)]);
+    float gate = 1.0f;                       // (ahead of the rows: the merge has no trip of its own)
+    if (MERGED && p.merge.gates) gate = p.merge.gates[(int64_t)(b * p.rr + (p.rr == 1 ? 0 : h0)) * p.k + min((lane & 7) / p.shard_waves, p.k - 1)];
     const int64_t be = (int64_t)b * p.E + e;
     const int n = min(__builtin_amdgcn_readlane(n_lane, e), p.S);
     auto address = [&](uint64_t of_lane) {
@@ -127,14 +178,16 @@ __global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void qu
         return reinterpret_cast<char *>(((uint64_t)hi << 32) | lo) + hk * p.stride_h;
     };
     int per = p.chunk;
-    if (p.nsplit_rcp != 0) {                 // cut by what the shard holds
+    if (!MERGED && p.nsplit_rcp != 0) {      // cut by what the shard holds
         constexpr int ROUND = kWaves * kTile;
         per = (int)__umulhi((uint32_t)(max(n, 0) + p.nsplit - 1), p.nsplit_rcp);
         per = min((max(per, 1) + ROUND - 1) / ROUND * ROUND, p.chunk);
     }
-    const int first = split * per, last = min(n, first + per);
+    // The wave's rows: stages of kTile rows at `start`, a round apart.
+    const int first = split * per, last = MERGED && j == p.k ? 0 : min(n, first + per);
+    const int start = first + (MERGED ? wave % p.shard_waves : wave) * kTile, round = (MERGED ? p.shard_waves : kWaves) * kTile;
     const int64_t part_base = (((int64_t)b * p.Hq + h0) * p.k + j) * p.nsplit + split, part_row = (int64_t)p.k * p.nsplit;
-    if (first >= last) {
+    if (!MERGED && first >= last) {
         for (int idx = tid; idx < rows * (W / 4); idx += kWaves * kWave) {
             const int g = idx / (W / 4), d = (idx - g * (W / 4)) * 4;
             const int64_t at = part_base + g * part_row;
@@ -162,19 +215,19 @@ __global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void qu
         return __builtin_amdgcn_make_buffer_rsrc(base + (int64_t)at * rb, 0, bytes, 0x00020000);
     };
     auto load_k = [&](int t0) {
-        sr = scales[min(t0 + 16 * (lane & 1), last - 1) >> p.block_bits];
+        sr = scales[max(min(t0 + 16 * (lane & 1), last - 1), 0) >> p.block_bits];
         const auto from = rsrc(Kb, t0);
         const uint32_t at = opaque(k_lane);
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
-            for (int u = 0; u < KU; ++u) buffer_load<KB>(kr[hb][u], from, at + 16 * hb * rb + 4 * KB * u);
+            for (int u = 0; u < KU; ++u) buffer_load<KB, true>(kr[hb][u], from, at + 16 * hb * rb + 4 * KB * u);
     };
     auto load_v = [&](int t0) {
         const auto from = rsrc(Vb, t0);
         const uint32_t at = opaque(v_lane);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) buffer_load<SETS>(vr[t], from, at + (16 * (t >> 2) + (t & 3)) * rb);
+        for (int t = 0; t < 8; ++t) buffer_load<SETS, W == 128>(vr[t], from, at + (16 * (t >> 2) + (t & 3)) * rb);
     };
 
     // Query operand of row tile rt, step s = (KB / 8) u + v: lane (c, r) holds values 4 KB u + KB r + 8 v + 0 .. 7 of its row c.
@@ -196,8 +249,8 @@ __global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void qu
             }
         }
     }
-    load_k(first + wave * kTile);
-    load_v(first + wave * kTile);
+    load_k(start);
+    load_v(start);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -215,7 +268,7 @@ __global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void qu
         for (int i = 0; i < SETS; ++i) acc[rt][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
 
-    for (int t0 = first + wave * kTile; t0 < last; t0 += kWaves * kTile) {
+    for (int t0 = start; t0 < last; t0 += round) {
         // scores sv[rt][4 hb + x]: entry t0 + 16 hb + 4 r + x, row c of row tile rt
         float sv[RT][8];
         const int scale_bits = __float_as_int(sr);
@@ -241,7 +294,7 @@ __global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void qu
                 for (int x = 0; x < 4; ++x) sv[rt][4 * hb + x] = sc[rt][x] * ks * p.scale;
         }
         const float vs0 = __int_as_float(__builtin_amdgcn_readlane(scale_bits, 2)), vs1 = __int_as_float(__builtin_amdgcn_readlane(scale_bits, 3));
-        load_k(t0 + kWaves * kTile);
+        load_k(t0 + round);
         if (t0 + kTile > last) {             // (uniform)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
@@ -297,29 +350,38 @@ __global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void qu
             split_bf16(sv[rt], pop[rt]);
         }
         // O^T += V^T P^T, output set i takes byte i of each of the lane's 8 V rows
-        const auto &v = vr;
 #pragma unroll
         for (int w = 0; w < (SETS + 3) / 4; ++w) {
             uint32_t lo[4], hi[4];
-            transpose4(v[0][w], v[1][w], v[2][w], v[3][w], lo);
-            transpose4(v[4][w], v[5][w], v[6][w], v[7][w], hi);
+            if constexpr (F == PIKV_QUANT_E4M3) {
+                transpose4(vr[0][w], vr[1][w], vr[2][w], vr[3][w], lo);
+                transpose4(vr[4][w], vr[5][w], vr[6][w], vr[7][w], hi);
+            }
 #pragma unroll
             for (int i = 0; i < (SETS < 4 ? SETS : 4); ++i) {
-                const uint4 vop = codes_operand<F>(lo[i], hi[i]);
+                uint4 vop;
+                if constexpr (F == PIKV_QUANT_E4M3) {
+                    vop = codes_operand<F>(lo[i], hi[i]);
+                } else {                     // (a conversion takes its byte from any place)
+                    auto pair = [&](int t) {
+                        const float a = (float)(int8_t)(vr[t][w] >> (8 * i)), b = (float)(int8_t)(vr[t + 1][w] >> (8 * i));
+                        return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+                    };
+                    vop = make_uint4(pair(0), pair(2), pair(4), pair(6));
+                }
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
+                for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                     for (int part = 2; part >= 0; --part) acc[rt][4 * w + i] = mfma_rows(vop, pop[rt][part], acc[rt][4 * w + i]);
-                }
             }
         }
-        load_v(t0 + kWaves * kTile);
+        load_v(t0 + round);
     }
 
     // waves -> LDS -> the block's partial, row tile by row tile (rows padded by 4 floats: banks)
     constexpr int AP = W + 4;
     extern __shared__ __attribute__((aligned(16))) float sm_acc[];       // [wave][row][AP], rows of a tile
-    __shared__ float sm_m[kWaves][kRows], sm_l[kWaves][kRows];
+    __shared__ float sm_m[WAVES][kRows], sm_l[WAVES][kRows], sm_f[WAVES][kRows];
     const int tile_rows = min(kRows, p.rows);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -340,16 +402,23 @@ __global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void qu
             sm_l[wave][c] = ls;
         }
         __syncthreads();
-        for (int idx = tid; idx < rows_here * (W / 4); idx += kWaves * kWave) {
+        if constexpr (MERGED) {
+            merge_rows(p, b, h0, hk, row0, rows_here, gate, sm_m, sm_l, sm_f);
+            __syncthreads();
+        }
+        for (int idx = tid; idx < rows_here * (W / 4); idx += WAVES * kWave) {
             const int g = idx / (W / 4), d = (idx - g * (W / 4)) * 4;
             float M = sm_m[0][g];
+            if constexpr (!MERGED) {
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm_m[w][g]);
+                for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sm_m[w][g]);
+            }
             float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
             float L = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float f = sm_m[w][g] == -INFINITY ? 0.0f : __expf(sm_m[w][g] - M);
+            for (int w = 0; w < WAVES; ++w) {
+                if (MERGED && w >= p.k * p.shard_waves) break;
+                const float f = MERGED ? sm_f[w][g] : sm_m[w][g] == -INFINITY ? 0.0f : __expf(sm_m[w][g] - M);
                 const float4 o = *reinterpret_cast<const float4 *>(sm_acc + (w * tile_rows + g) * AP + d);
                 a.x = fmaf(o.x, f, a.x);
                 a.y = fmaf(o.y, f, a.y);
@@ -357,9 +426,14 @@ __global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void qu
                 a.w = fmaf(o.w, f, a.w);
                 L = fmaf(sm_l[w][g], f, L);
             }
-            const int64_t at = part_base + (rt * kRows + g) * part_row;
-            *reinterpret_cast<float4 *>(p.part_acc + at * W + d) = a;
-            if (d == 0) *reinterpret_cast<float2 *>(p.part_ml + at * 2) = make_float2(M, L);
+            if constexpr (MERGED) {
+                float *to = p.merge.y + query_row(p, b, hk, row0 + g) * W + d;      // (y need not be 16-byte aligned)
+                to[0] = a.x, to[1] = a.y, to[2] = a.z, to[3] = a.w;
+            } else {
+                const int64_t at = part_base + (rt * kRows + g) * part_row;
+                *reinterpret_cast<float4 *>(p.part_acc + at * W + d) = a;
+                if (d == 0) *reinterpret_cast<float2 *>(p.part_ml + at * 2) = make_float2(M, L);
+            }
         }
     }
 }
@@ -367,6 +441,7 @@ __global__ __launch_bounds__(kWaves *kWave, quant_blocks_per_cu(RT, QP)) void qu
 struct QuantPlan {
     int row_tiles, rows, row_blocks;      // matrix tiles and query rows of a block; row blocks of a kv head
     int nsplit, chunk;
+    bool merged;               // one launch, no partials
     size_t acc_bytes, ml_bytes;
 };
 
@@ -383,10 +458,17 @@ int make_plan(const pikv_desc *d, int k, QuantPlan *plan) {
     plan->rows = per_head ? 1 : G < plan->row_tiles * kRows ? G : plan->row_tiles * kRows;
     plan->row_blocks = (G + plan->rows - 1) / plan->rows;
     const int64_t units = (int64_t)d->B * d->Hkv * plan->row_blocks * k;
+    // The merged form, one launch and no partials: where a wave's rows are one stage or two (1 x 8 kv heads x 2 of 128 entries 7.9 -> 6.7 us, 256
+    // entries, two stages of a wave, even) and where there are blocks for most CUs without splits (64 x 8 x 2 of 64 - 1000 entries 14.5 -> 9.7 to
+    // 53.8 -> 49.0; 16 x 8 x 2 of 4096 40 -> 61), but not many short ones (2048 blocks of 256 entries 32.2 -> 35.5).
+    const int64_t blocks = units / k, rows = (int64_t)k * d->S;
+    const bool one_round = (int64_t)d->S * d->D <= (int64_t)128 * kTile * (kMergedWaves / k);
+    plan->merged = plan->row_tiles == 1 && k <= kMergedWaves && blocks <= 640 && (one_round || (blocks >= 192 && rows <= 4096));
     // A block per CU, and blocks of at most 1024 rows, but none of fewer than a stage of each wave.
     int64_t nsplit = units > 0 ? 256 / units : 1;
     const int64_t finer = (d->S + kLongestBlock - 1) / kLongestBlock, most = (d->S + kWaves * kTile - 1) / (kWaves * kTile);
     if (nsplit < finer) nsplit = finer;
+    if (plan->merged) nsplit = 1;
     if (nsplit > most) nsplit = most;
     if (nsplit > kMaxPartialsPerHead / k) nsplit = kMaxPartialsPerHead / k;
     if (nsplit < 1) nsplit = 1;
@@ -464,6 +546,8 @@ extern "C" int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t bl
     p.block_bits = __builtin_ctz(block);
     p.nsplit_rcp = plan.nsplit > 1 ? (uint32_t)(((uint64_t)1 << 32) / plan.nsplit + 1) : 0u;
     p.scale = scale > 0.0f ? scale : 1.0f / sqrtf((float)desc->D);
+    p.shard_waves = kMergedWaves / k;
+    p.merge = {gates, y, row_max, row_norm, slot_coef, combine};
     CombineParams c;
     c.part_acc = p.part_acc;
     c.part_ml = p.part_ml;
@@ -486,15 +570,26 @@ extern "C" int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t bl
     c.by_Hq = fast_div(c.Hq);
     c.by_G = fast_div(c.G);
     c.decoder_bytes = 0;
-    const dim3 grid((unsigned)((int64_t)desc->B * desc->Hkv * plan.row_blocks * k * plan.nsplit)), threads(kWaves * kWave);
-    const size_t lds = (size_t)kWaves * (plan.rows < kRows ? plan.rows : kRows) * (desc->D + 4) * sizeof(float);
+    const int waves = plan.merged ? kMergedWaves : kWaves;
+    const dim3 grid((unsigned)((int64_t)desc->B * desc->Hkv * plan.row_blocks * (plan.merged ? 1 : k * plan.nsplit))), threads(waves * kWave);
+    const size_t lds = (size_t)waves * (plan.rows < kRows ? plan.rows : kRows) * (desc->D + 4) * sizeof(float);
     hipStream_t st = as_stream(stream);
     auto launch = [&](auto width, auto fmt) {
         constexpr int W = decltype(width)::value, F = decltype(fmt)::value;
         auto go = [&](auto parts, auto tiles) {
             constexpr int QP = decltype(parts)::value, RT = decltype(tiles)::value;
-            if (scores) hipLaunchKernelGGL((quant_attn_partial<W, F, QP, RT, true>), grid, threads, lds, st, p);
-            else hipLaunchKernelGGL((quant_attn_partial<W, F, QP, RT, false>), grid, threads, lds, st, p);
+            auto scored = [&](auto with) {
+                constexpr bool SC = decltype(with)::value;
+                if constexpr (RT == 1) {
+                    if (plan.merged) {
+                        hipLaunchKernelGGL((quant_attn_partial<W, F, QP, RT, SC, kMergedWaves>), grid, threads, lds, st, p);
+                        return;
+                    }
+                }
+                hipLaunchKernelGGL((quant_attn_partial<W, F, QP, RT, SC, kWaves>), grid, threads, lds, st, p);
+            };
+            if (scores) scored(std::true_type{});
+            else scored(std::false_type{});
         };
         const std::integral_constant<int, 1> one{};
         if (desc->dtype == PIKV_F32) go(std::integral_constant<int, 3>{}, one);
@@ -509,6 +604,6 @@ extern "C" int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t bl
     if (format == PIKV_QUANT_INT8) by_width(std::integral_constant<int, PIKV_QUANT_INT8>{});
     else by_width(std::integral_constant<int, PIKV_QUANT_E4M3>{});
     rc = launch_status();
-    if (rc != PIKV_OK) return rc;
+    if (rc != PIKV_OK || plan.merged) return rc;
     return pikv_sharded_attn_merge(desc, &c, stream);
 }

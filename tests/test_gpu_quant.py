@@ -365,6 +365,38 @@ def test_draft_queries_in_the_tokens_layout(spec):
     a.check()
 
 
+@pytest.mark.parametrize("dtype,fmt", [("bf16", INT8), ("f32", E4M3)], ids=["bf16_int8", "f32_e4m3"])
+@pytest.mark.parametrize("k", range(1, 9))
+def test_short_shards_whose_waves_share_a_block(k, dtype, fmt):
+    """8 waves over k shards: 8, 4, 2 or 1 each, some left over; shards without entries, rows without any."""
+    n = np.random.default_rng(k).integers(0, 41, (3, 9)) * (np.random.default_rng(k + 50).random((3, 9)) < 0.7)
+    n[2] = 0
+    a = Attn(3, 12, 4, [128, 64][k % 2], 9, 40, k, dtype=dtype, fmt=fmt, block=16, n=n, seed=k, gates=k != 4)
+    for combine in (pk.COMBINE_LSE, pk.COMBINE_LOCAL):
+        a.run(combine)
+        want = a.check(combine)
+        u = torch.rand((3, 9, 40), device=DEV)
+        after = u.clone()
+        pk.pikv_update_utility(a.cache.desc, a.scores, a.coef, a.d["n"], a.d["topk"], k, 0.5, after)
+        visited = np.zeros((3, 9, 1), bool)
+        for b in range(3):
+            visited[b, a.topk[b]] = True
+        live = (np.arange(40) < n[..., None]) & visited
+        u = u.cpu().numpy().astype(np.float64)
+        np.testing.assert_allclose(after.cpu().numpy(), np.where(live, 0.5 * u + want["mass"], u), rtol=1e-4, atol=1e-9)
+
+
+@pytest.mark.parametrize("spec", [dict(B=48, Hq=8, Hkv=4, D=64, E=3, S=300, k=3), dict(B=47, Hq=8, Hkv=4, D=64, E=3, S=300, k=3),
+                                  dict(B=100, Hq=2, Hkv=2, D=128, E=2, S=130, k=2, dtype="f32"), dict(B=25, Hq=8, Hkv=8, D=32, E=4, S=150, k=1, per_head=True),
+                                  dict(B=40, Hq=60, Hkv=5, D=64, E=2, S=90, k=2, tq=4, fmt=E4M3), dict(B=161, Hq=4, Hkv=4, D=32, E=2, S=33, k=1)],
+                         ids=lambda s: "B%d_Hkv%d_S%d" % (s["B"], s["Hkv"], s["S"]))
+def test_many_sequences(spec):
+    """Enough (sequence, kv head) pairs for a block each, and one fewer."""
+    a = Attn(**spec, seed=12)
+    a.run()
+    a.check()
+
+
 def test_strided_rows_a_given_scale_and_a_query_that_is_not_aligned():
     a = Attn(2, 12, 3, 64, 3, 170, 2, pad=48, gap=7, seed=7)
     q = torch.zeros(a.d["q"].numel() + 1, device=DEV, dtype=torch.bfloat16)[1:].view(a.d["q"].shape)
