@@ -404,14 +404,15 @@ int pikv_norm_rope(const void *x, int32_t tokens, int64_t token_stride, int32_t 
  *   format  pikv_quant_format; block: 16, 32, 64 or 128 slots that share a scale
  *   K_scales, V_scales [B,E,Hkv,ceil(S/block)] float32: one scale per block of slots
  *           and kv head, K and V apart.  Entry i of a row stands for code_i * scale.
- * Scales are powers of two: the smallest one, 2^-126 at the least, that brings the largest magnitude of
- * the block's rows within the largest code (127 or 448).  Divisions by it are then exact, a code is the nearest
- * one (ties to even) to x / scale, and the value it stands for is exact in either dense type unless that underflows
- * - every call here gives the same bits on every machine.  A block that is given a NaN or an infinity has a NaN scale
- * and reads as NaN until it is written anew.
- * pikv_route, pikv_evict with compact == 0, pikv_policy_stamp, pikv_policy_utility and the utility updates serve these
- * shards as they are; pikv_evict with compact != 0 moves rows of the dense type and must not be used
- * on them, nor pikv_append, pikv_sharded_attn or the fused steps.                                                   */
+ * Scales are powers of two (or 0 where nothing has been written: zeros): the smallest one, 2^-126 at
+ * the least, that brings the largest magnitude of the block's rows within the largest code (127 or 448).
+ * Divisions by it are then exact, a code is the nearest one (ties to even) to x / scale, and the value it
+ * stands for is exact in either dense type unless it underflows - every call here gives the same bits on
+ * every machine.  A block that is given a NaN or an infinity has a NaN scale and reads as NaN until it is
+ * written anew.
+ * pikv_route, pikv_evict with compact == 0, pikv_policy_stamp, pikv_policy_utility and the utility updates
+ * serve these shards as they are; pikv_evict with compact != 0 moves rows of the dense type and must not be
+ * used on them, nor pikv_append, pikv_sharded_attn or the fused steps.                                   */
 typedef enum { PIKV_QUANT_INT8 = 0, PIKV_QUANT_E4M3 = 1 } pikv_quant_format;
 
 /* Writes shards from dense ones: codes of the entries 0 .. n_valid[b][e]-1 (at most S) and the scales of the blocks
@@ -452,7 +453,8 @@ size_t pikv_quant_attn_workspace_bytes(const pikv_desc *desc, int32_t k);
 
 /* pikv_sharded_attn over these shards: same meaning of every argument, both combine modes, per-token and per-head
  * routing; desc->tq > 1 (the multi-query layout above) for either dtype, every D here and any group size.  Scores and sums are
- * those of the values code * scale, exact to fp32 accumulation.  scores + slot_coef feed pikv_update_utility.
+ * those of the values code * scale, exact to fp32 accumulation.  scores + slot_coef feed pikv_update_utility.  The
+ * workspace holds nothing between calls; calls that may overlap (streams, captured graphs) need one each.
  * Errors: as pikv_sharded_attn; UNSUPPORTED as above, for tq > 1 with per-head routing, stride_s above 2^24 bytes and
  * 2^23 blocks of work or more.                                                                   */
 int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t block, const void *q,

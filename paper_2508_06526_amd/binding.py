@@ -509,10 +509,11 @@ def _on_device(where, call, stream, *tensors):
         return call(_stream(stream))
 
 
-def _int32_float32(where, integers, floats):
+def _int32_float32(where, integers, floats, tables=()):
     import torch
     _typed(where, torch.int32, *integers)
     _typed(where, torch.float32, *floats)
+    _typed(where, torch.int64, *tables)          # of shard addresses, not the shards
 
 
 def _rows(x, token_stride):
@@ -548,7 +549,7 @@ def pikv_quant_pack(desc, format, block, K_dense, V_dense, dense_stride_h, dense
     st = _calls().pikv_quant_pack(desc, format, block, K_dense, V_dense, dense_stride_h, dense_stride_s, n_valid, K_shards, V_shards,
                                   K_scales, V_scales, _raw(stream))
     if st is None:
-        _int32_float32(where, [n_valid], [K_scales, V_scales])
+        _int32_float32(where, [n_valid], [K_scales, V_scales], [K_dense, V_dense, K_shards, V_shards])
         st = _on_device(where, lambda s: load_library().pikv_quant_pack(
             C.byref(desc), format, block, _p(K_dense), _p(V_dense), dense_stride_h, dense_stride_s, _p(n_valid), _p(K_shards),
             _p(V_shards), _p(K_scales), _p(V_scales), s), stream, K_dense, V_dense, n_valid, K_shards, V_shards, K_scales, V_scales)
@@ -562,7 +563,7 @@ def pikv_quant_read(desc, format, block, K_shards, V_shards, K_scales, V_scales,
     st = _calls().pikv_quant_read(desc, format, block, K_shards, V_shards, K_scales, V_scales, n_valid, K_dense, V_dense,
                                   dense_stride_h, dense_stride_s, _raw(stream))
     if st is None:
-        _int32_float32(where, [n_valid], [K_scales, V_scales])
+        _int32_float32(where, [n_valid], [K_scales, V_scales], [K_dense, V_dense, K_shards, V_shards])
         st = _on_device(where, lambda s: load_library().pikv_quant_read(
             C.byref(desc), format, block, _p(K_shards), _p(V_shards), _p(K_scales), _p(V_scales), _p(n_valid), _p(K_dense),
             _p(V_dense), dense_stride_h, dense_stride_s, s), stream, K_shards, V_shards, K_scales, V_scales, n_valid, K_dense, V_dense)
@@ -577,7 +578,7 @@ def pikv_quant_append(desc, format, block, K_new, V_new, topk_idx, k, reuse_idx,
     st = _calls().pikv_quant_append(desc, format, block, K_new, V_new, topk_idx, k, reuse_idx, reuse_cnt, max_evict, K_shards,
                                     V_shards, K_scales, V_scales, utility, n_valid, _raw(stream))
     if st is None:
-        _int32_float32(where, [topk_idx, reuse_idx, reuse_cnt, n_valid], [K_scales, V_scales, utility])
+        _int32_float32(where, [topk_idx, reuse_idx, reuse_cnt, n_valid], [K_scales, V_scales, utility], [K_shards, V_shards])
         st = _on_device(where, lambda s: load_library().pikv_quant_append(
             C.byref(desc), format, block, _p(K_new), _p(V_new), _p(topk_idx), k, _p(reuse_idx), _p(reuse_cnt), max_evict,
             _p(K_shards), _p(V_shards), _p(K_scales), _p(V_scales), _p(utility), _p(n_valid), s),
@@ -597,7 +598,8 @@ def pikv_quant_attn(desc, format, block, q, K_shards, V_shards, K_scales, V_scal
     st = _calls().pikv_quant_attn(desc, format, block, q, K_shards, V_shards, K_scales, V_scales, n_valid, topk_idx, gates, k, combine,
                                   scale, y, row_max, row_norm, scores, slot_coef, workspace, _raw(stream))
     if st is None:
-        _int32_float32(where, [n_valid, topk_idx], [K_scales, V_scales, gates, y, row_max, row_norm, scores, slot_coef])
+        _int32_float32(where, [n_valid, topk_idx], [K_scales, V_scales, gates, y, row_max, row_norm, scores, slot_coef],
+                       [K_shards, V_shards])
         ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
         st = _on_device(where, lambda s: load_library().pikv_quant_attn(
             C.byref(desc), format, block, _p(q), _p(K_shards), _p(V_shards), _p(K_scales), _p(V_scales), _p(n_valid), _p(topk_idx),

@@ -56,7 +56,7 @@ struct Args {
     const at::Tensor *last = nullptr;    // the last tensor taken
     const at::Tensor *first = nullptr;
     bool usual = true;                   // every argument so far was of the ordinary kind (no exception: one costs as much as a call)
-    bool strict = false;                 // the tensors of int32_t * and float * are of that type, and all are on one device
+    bool strict = false;                 // the tensors of int32_t *, float * and tables are of that type (tables: int64), and all are on one device
 
     template <typename T>
     T unusual() {
@@ -97,7 +97,8 @@ struct Take {
             const at::Tensor *t = a.tensor(o);
             typedef std::remove_const_t<std::remove_pointer_t<T>> Element;
             if (a.strict && t != nullptr && ((std::is_same_v<Element, int32_t> && t->scalar_type() != at::kInt) ||
-                                             (std::is_same_v<Element, float> && t->scalar_type() != at::kFloat)))
+                                             (std::is_same_v<Element, float> && t->scalar_type() != at::kFloat) ||
+                                             (std::is_pointer_v<Element> && t->scalar_type() != at::kLong)))
                 return a.template unusual<T>();
             a.last = t;
             if (a.first == nullptr) a.first = t;

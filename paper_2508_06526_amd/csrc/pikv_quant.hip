@@ -215,9 +215,10 @@ __global__ __launch_bounds__(1024) void quant_append(QuantAppendParams p) {
         if (others) scale = max(scale, old);
         const float inv = inverse_scale(scale);
         if (others && scale != old) {
-            // old / scale, at most 1/2; 0 from where it underflows, and codes with it (NaN scale: 0)
+            // old / scale, at most 1/2; 0 from where it underflows, and codes with it (NaN scale: 0; so an old scale of 0, whose
+            // codes stand for zeros)
             const int shift = (int)(scale >> 23) - (int)(old >> 23);
-            const float ratio = scale >= 0x7f800000u || shift > 126 ? 0.0f : __uint_as_float((uint32_t)(127 - shift) << 23);
+            const float ratio = scale >= 0x7f800000u || old == 0 || shift > 126 ? 0.0f : __uint_as_float((uint32_t)(127 - shift) << 23);
             constexpr int kAtOnce = 8;
             for (int s0 = lo; s0 < hi; s0 += kAtOnce) {
                 uint2 w[kAtOnce];

@@ -243,6 +243,17 @@ def test_append_without_freed_slots_and_a_poisoned_block():
     assert np.isnan(scales[0][0, 0, 1, 1]) and np.isfinite(scales[0][0, 0, 1, [0, 2]]).all() and np.isfinite(scales[0][0, 0, 0]).all()
 
 
+def test_append_into_a_block_of_zeros_that_was_never_written():
+    cache = Cache(1, 1, 2, 32, 64, "f32", E4M3, 16, fill=0x3C)          # (bytes that stand for nothing: their scale is 0)
+    for s in cache.scales:
+        s.zero_()
+    n, u, rows = i32([[5]]), torch.zeros((1, 1, 32), device=DEV), up(np.random.default_rng(2).normal(size=(1, 2, 64)))
+    assert all((t[0, 0, :, :5] == 0).all() for t in cache.read([[5]]))
+    pk.pikv_quant_append(cache.desc, E4M3, 16, rows, rows, i32([[0]]), 1, None, None, 0, *cache.tabs, *cache.scales, u, n)
+    after = cache.read([[6]])
+    assert all((t[0, 0, :, :5] == 0).all() and (t[0, 0, :, 5] != 0).any() for t in after)
+
+
 # ------------------------------------------------------------------------------ attention
 class Attn:
     def __init__(self, B, Hq, Hkv, D, E, S, k, dtype="bf16", fmt=INT8, block=32, per_head=False, tq=1, n=None, seed=0, pad=0, gap=0, gates=True,

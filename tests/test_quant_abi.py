@@ -96,17 +96,20 @@ def test_the_binding_refuses_host_memory_and_other_types(name):
     d, f = desc(), lambda *shape, t=torch.float32: torch.zeros(shape, dtype=t)
     i32, tab, bf = f(4, t=torch.int32), f(16, t=torch.int64), f(16, t=torch.bfloat16)
     calls = {
-        "pikv_norm_rope": lambda i, s: pk.pikv_norm_rope(bf, 1, 512, 4, 2, 64, None, None, 1e-6, i, s, 64, False, bf, bf, bf),
-        "pikv_quant_pack": lambda i, s: pk.pikv_quant_pack(d, 0, 16, tab, tab, 6400, 64, i, tab, tab, s, s),
-        "pikv_quant_read": lambda i, s: pk.pikv_quant_read(d, 0, 16, tab, tab, s, s, i, tab, tab, 6400, 64),
-        "pikv_quant_append": lambda i, s: pk.pikv_quant_append(d, 0, 16, bf, bf, i, 2, i, i, 1, tab, tab, s, s, s, i),
-        "pikv_quant_attn": lambda i, s: pk.pikv_quant_attn(d, 0, 16, bf, tab, tab, s, s, i, i, s, 2, 0, 0.0, s, s, s, s, s, s)}
+        "pikv_norm_rope": lambda i, s, tab=tab: pk.pikv_norm_rope(bf, 1, 512, 4, 2, 64, None, None, 1e-6, i, s, 64, False, bf, bf, bf),
+        "pikv_quant_pack": lambda i, s, tab=tab: pk.pikv_quant_pack(d, 0, 16, tab, tab, 6400, 64, i, tab, tab, s, s),
+        "pikv_quant_read": lambda i, s, tab=tab: pk.pikv_quant_read(d, 0, 16, tab, tab, s, s, i, tab, tab, 6400, 64),
+        "pikv_quant_append": lambda i, s, tab=tab: pk.pikv_quant_append(d, 0, 16, bf, bf, i, 2, i, i, 1, tab, tab, s, s, s, i),
+        "pikv_quant_attn": lambda i, s, tab=tab: pk.pikv_quant_attn(d, 0, 16, bf, tab, tab, s, s, i, i, s, 2, 0, 0.0, s, s, s, s, s, s)}
     with pytest.raises(ValueError, match="device memory"):
         calls[name](i32, f(4))
     with pytest.raises(TypeError, match="int32"):
         calls[name](i32.long(), f(4))
     with pytest.raises(TypeError, match="float32"):
         calls[name](i32, f(4, t=torch.float64))
+    if name != "pikv_norm_rope":                 # the shards in place of the table of their addresses
+        with pytest.raises(TypeError, match="int64"):
+            calls[name](i32, f(4), tab=f(16, t=torch.uint8))
 
 
 def test_the_binding_refuses_dense_tensors_of_another_type():
