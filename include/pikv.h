@@ -389,9 +389,9 @@ int pikv_policy_compact(const pikv_desc *desc, const int32_t *evicted_idx, const
  *             Outputs must not overlap x or each other.
  * Hq or Hkv may be 0 (separate projections); q_out or k_out may then be NULL.
  * Errors: INVALID for null required pointers, tokens < 0, Hq or Hkv < 0 or both 0, token_stride too
- * small, x, weights or outputs that are not 16-byte aligned, rotary_dim not in 0..D or no multiple of 16, eps < 0 or
- * not finite, unknown dtype; UNSUPPORTED for D other than 16, 32, 64, 128 and for more than 2^23 blocks
- * (tokens * heads / 16 of 128 values).  tokens == 0 is a no-op.                                           */
+ * small, x, weights or outputs that are not 16-byte aligned, rotary_dim not in 0..D or no multiple of 16,
+ * eps < 0 or not finite, unknown dtype; UNSUPPORTED for D other than 16, 32, 64, 128 and for more than
+ * 2^20 heads or 2^23 tokens.  tokens == 0 is a no-op.                                                    */
 int pikv_norm_rope(const void *x, int32_t tokens, int64_t token_stride, int32_t Hq, int32_t Hkv, int32_t D,
                    int32_t dtype, const void *w_q, const void *w_k, float eps, const int32_t *positions,
                    const float *inv_freq, int32_t rotary_dim, int32_t interleaved, void *q_out, void *k_out,
@@ -415,33 +415,34 @@ int pikv_norm_rope(const void *x, int32_t tokens, int64_t token_stride, int32_t 
  * used on them, nor pikv_append, pikv_sharded_attn or the fused steps.                                   */
 typedef enum { PIKV_QUANT_INT8 = 0, PIKV_QUANT_E4M3 = 1 } pikv_quant_format;
 
-/* Writes shards from dense ones: codes of the entries 0 .. n_valid[b][e]-1 (at most S) and the scales of the blocks
- * they lie in; everything behind them is left as it was, and dense rows behind them are not read.
+/* Writes shards from dense ones: codes of the entries 0 .. n_valid[b][e]-1 (at most S) and the scales of the
+ * blocks they lie in; everything behind them is left as it was, and dense rows behind them are not read.
  *   K_dense, V_dense  device tables of B*E shards of dtype, rows at h' * dense_stride_h + slot * dense_stride_s
  *                     elements, on 16-byte boundaries
- * Errors: descriptor errors, UNSUPPORTED as above and for 2^23 blocks of work or more (64 slots of a kv head's K or V
- * each; 128 with block 128), INVALID for null pointers, unknown format, block other than the four, dense strides below D or
- * not multiples of 16 bytes.  B == 0 is a no-op.                                                    */
+ * Errors: descriptor errors, UNSUPPORTED as above and for 2^23 blocks of work or more (64 slots of a kv head's
+ * K or V each; 128 with block 128), INVALID for null pointers, unknown format, block other than the four, dense
+ * strides that do not hold the rows or are not multiples of 16 bytes.  B == 0 is a no-op.                */
 int pikv_quant_pack(const pikv_desc *desc, int32_t format, int32_t block, const void *const *K_dense,
                     const void *const *V_dense, int64_t dense_stride_h, int64_t dense_stride_s,
                     const int32_t *n_valid, void *const *K_shards, void *const *V_shards, float *K_scales,
                     float *V_scales, void *stream);
 
-/* Reads them back: dense rows 0 .. n_valid[b][e]-1 = code * scale, rounded to the dense type; rows behind them are left
- * as they were.  Arguments and errors as pikv_quant_pack.                                                     */
+/* Reads them back: dense rows 0 .. n_valid[b][e]-1 = code * scale, rounded to the dense type; rows behind them
+ * are left as they were.  Arguments and errors as pikv_quant_pack.                                       */
 int pikv_quant_read(const pikv_desc *desc, int32_t format, int32_t block, const void *const *K_shards,
                     const void *const *V_shards, const float *K_scales, const float *V_scales,
                     const int32_t *n_valid, void *const *K_dense, void *const *V_dense, int64_t dense_stride_h,
                     int64_t dense_stride_s, void *stream);
 
-/* pikv_append for these shards: the same slot rule, utility and count; the new rows [B,Hkv,D] dtype become codes.  If
- * other live slots share the block, its scale is the larger of its own and the one the new row needs, and where
- * that is larger than its own their codes are rounded to it; else (the block's first entry) it is the new row's.  A
- * scale does not shrink when the entry that set it leaves.  Live slots are those below n_valid + 1 or, with
- * reuse_cnt[b][e] = c > 1 freed slots, below n_valid + c; no other row's codes are touched.
- * Errors: descriptor errors, UNSUPPORTED as above, INVALID for null required pointers, unknown format or block,
- * k not in 1..E, one of reuse_idx and reuse_cnt without the other, max_evict < 1 with them.  Per-token routing only
- * (UNSUPPORTED otherwise).                                                                               */
+/* pikv_append for these shards: the same slot rule, utility and count; the new rows [B,Hkv,D] dtype become
+ * codes.  If other live slots share the block, its scale is the larger of its own and the one the new row
+ * needs, and where that is larger than its own their codes are rounded to it; else (the block's first entry)
+ * it is the new row's.  A scale does not shrink when the entry that set it leaves.  Live slots are those below
+ * n_valid + 1 or, with reuse_cnt[b][e] = c > 1 freed slots, below n_valid + c; no other row's codes are
+ * touched.  A shard listed twice in a row of topk_idx takes the entry once.
+ * Errors: descriptor errors, UNSUPPORTED as above and for B * k > 2^21, INVALID for null required pointers,
+ * unknown format or block, k not in 1..E, one of reuse_idx and reuse_cnt without the other, max_evict < 1 with
+ * them.  Per-token routing only (UNSUPPORTED otherwise).                                                  */
 int pikv_quant_append(const pikv_desc *desc, int32_t format, int32_t block, const void *K_new, const void *V_new,
                       const int32_t *topk_idx, int32_t k, const int32_t *reuse_idx, const int32_t *reuse_cnt,
                       int32_t max_evict, void *const *K_shards, void *const *V_shards, float *K_scales,
@@ -451,12 +452,13 @@ int pikv_quant_append(const pikv_desc *desc, int32_t format, int32_t block, cons
  * The workspace must be 256-byte aligned.                                                                 */
 size_t pikv_quant_attn_workspace_bytes(const pikv_desc *desc, int32_t k);
 
-/* pikv_sharded_attn over these shards: same meaning of every argument, both combine modes, per-token and per-head
- * routing; desc->tq > 1 (the multi-query layout above) for either dtype, every D here and any group size.  Scores and sums are
- * those of the values code * scale, exact to fp32 accumulation.  scores + slot_coef feed pikv_update_utility.  The
- * workspace holds nothing between calls; calls that may overlap (streams, captured graphs) need one each.
- * Errors: as pikv_sharded_attn; UNSUPPORTED as above, for tq > 1 with per-head routing, stride_s above 2^24 bytes and
- * 2^23 blocks of work or more.                                                                   */
+/* pikv_sharded_attn over these shards: same meaning of every argument, both combine modes, per-token and
+ * per-head routing; desc->tq > 1 (the multi-query layout above) for either dtype, every D here and any group
+ * size.  Scores and sums are those of the values code * scale, exact to fp32 accumulation; scores + slot_coef
+ * feed pikv_update_utility.  A selected index outside 0..E-1 counts as an empty shard here.  The workspace holds
+ * nothing between calls; calls that may overlap (streams, captured graphs) need one each.
+ * Errors: as pikv_sharded_attn; UNSUPPORTED as above, for tq > 1 with per-head routing, stride_s above 2^24
+ * bytes and 2^23 blocks of work or more.                                                                 */
 int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t block, const void *q,
                     const void *const *K_shards, const void *const *V_shards, const float *K_scales,
                     const float *V_scales, const int32_t *n_valid, const int32_t *topk_idx, const float *gates,

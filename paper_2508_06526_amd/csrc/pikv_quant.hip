@@ -194,6 +194,8 @@ __global__ __launch_bounds__(1024) void quant_append(QuantAppendParams p) {
     const int slot = cnt > 0 ? __builtin_amdgcn_readlane(idx_lane, e) : n;
     __syncthreads();                         // every thread has read n before it changes
     if (n >= p.S || slot < 0 || slot >= p.S) return;   // full shard: the entry is dropped
+    // A shard listed twice takes the entry once: two blocks rounding one block's codes would round them twice.
+    if (e < 0 || e >= p.E || __ballot(sel == e && lane < j) != 0) return;
     const int64_t be = be0 + e;
     const int blk = slot >> p.block_bits, lo = blk << p.block_bits;
     const int live = min(p.S, n + max(cnt, 1)), hi = min(lo + (1 << p.block_bits), live);      // live slots of the block: lo .. hi - 1

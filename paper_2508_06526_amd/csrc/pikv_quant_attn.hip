@@ -2,7 +2,8 @@
 // flash-decode on the matrix cores:
 //
 //   quant_attn_partial : grid over (sequence, kv head and its rows, selected shard, split), 4 waves a block; one (max, sum,
-//                        acc[D]) partial per row and block, in the layout of the merge that pikv_sharded_attn uses too.
+//                        acc[D]) partial per row and block, in the layout of the merge that pikv_sharded_attn uses too.  Short calls:
+//                        a block of 8 waves for all shards of its rows, merge included.
 //
 // A code is exact in bf16, so the products are those of the codes, and the scales - one per 16 slots or more, the same for
 // all lanes - multiply what comes out: a score by its K block's scale, a weight by its V block's before it meets the codes.
@@ -15,6 +16,12 @@
 //     operand P^T of the second product (three bf16 parts: all 24 bits).
 //   * O^T[d][row] += V^T . P^T: lane (c, r) loads D / 16 bytes of those 8 entries' rows; output set i takes the i-th byte of
 //     each.
+// A lane's piece of the next stage is requested as soon as this one's has been used: K behind the scores, V behind the output.
+//
+// Bound by memory from some 100 MB of codes on: 32 sequences x 32 kv heads x 2 shards of 2048 x 128 codes, 1.07 GB, in 166 us (6.5 TB/s; a pass
+// that only reads 156).  Below by the trips and launches around it: 64 MB under 4 query heads, with 4 MB of scores, 16.7 us
+// (the loads alone 14.2, a read-only pass 12.1) and a merge of 4.  Two stages ahead instead of one, or eight waves a block, changed
+// nothing but the registers.
 #include "pikv_combine_dev.h"
 #include "pikv_mfma_dev.h"
 #include "pikv_quant_dev.h"
@@ -28,8 +35,8 @@ constexpr int kWaves = 4;
 constexpr int kRows = 16;               // query rows of a matrix tile
 constexpr int kMergedWaves = 8;         // of a block that takes all shards of its rows
 constexpr int kTile = 32;               // entries of a stage of a wave
-// Row tiles of a block, at most.  (Four fit a CU once, with their accumulators moved to and fro: 64 rows over 128 MiB's worth of
-// 32K entries 26.5 us, as two blocks of two, the second reading from the caches, 22.7, as four of one 25.9; 32 rows: 23.7, 28.7.)
+// Row tiles of a block, at most.  (Four fit a CU once, with their accumulators moved to and fro: 64 rows over 32K entries of each of 4
+// kv heads 26.5 us, as two blocks of two, the second reading from the caches, 22.7, as four of one 25.9; 32 rows in blocks of two 23.7, of one 28.7.)
 constexpr int kMostTiles = 2;
 constexpr int kLongestBlock = 1024;     // rows of a block, while the merge holds the partials
 
@@ -168,11 +175,12 @@ __global__ __launch_bounds__(WAVES *kWave, WAVES == kWaves ? quant_blocks_per_cu
     const int64_t be_lane = (int64_t)b * p.E + min(lane, p.E - 1);
     const int n_lane = p.n_valid[be_lane];
     const uint64_t K_lane = reinterpret_cast<uint64_t>(p.K[be_lane]), V_lane = reinterpret_cast<uint64_t>(p.V[be_lane]);
-    const int e = __builtin_amdgcn_readfirstlane(p.topk[(int64_t)(b * p.rr + (p.rr == 1 ? 0 : h0)) * p.k + min(j, p.k - 1)]);
+    const int sel = __builtin_amdgcn_readfirstlane(p.topk[(int64_t)(b * p.rr + (p.rr == 1 ? 0 : h0)) * p.k + min(j, p.k - 1)]);
+    const int e = min(max(sel, 0), p.E - 1);
     float gate = 1.0f;                       // (ahead of the rows: the merge has no trip of its own)
     if (MERGED && p.merge.gates) gate = p.merge.gates[(int64_t)(b * p.rr + (p.rr == 1 ? 0 : h0)) * p.k + min((lane & 7) / p.shard_waves, p.k - 1)];
     const int64_t be = (int64_t)b * p.E + e;
-    const int n = min(__builtin_amdgcn_readlane(n_lane, e), p.S);
+    const int n = sel == e ? min(__builtin_amdgcn_readlane(n_lane, e), p.S) : 0;      // (no such shard: empty)
     auto address = [&](uint64_t of_lane) {
         const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)of_lane, e), hi = __builtin_amdgcn_readlane((int)(uint32_t)(of_lane >> 32), e);
         return reinterpret_cast<char *>(((uint64_t)hi << 32) | lo) + hk * p.stride_h;

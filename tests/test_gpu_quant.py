@@ -313,8 +313,8 @@ class Attn:
         rm, rn = self.row_max.cpu().numpy(), self.row_norm.cpu().numpy()
         empty = want["row_max"] == -np.inf
         assert (rm[empty] == -np.inf).all() and (rn[empty] == 0).all() and (y[empty] == 0).all()
-        assert (np.abs(rm - want["row_max"])[~empty] <= ds).all()
-        assert (np.abs(rn - want["row_norm"])[~empty] <= (w + 2.0 ** -20) * want["row_norm"][~empty]).all()
+        assert (np.abs(rm[~empty] - want["row_max"][~empty]) <= ds).all()
+        assert (np.abs(rn[~empty] - want["row_norm"][~empty]) <= (w + 2.0 ** -20) * want["row_norm"][~empty]).all()
         if scores:
             got = self.scores.cpu().numpy()
             live = ~np.isnan(want["scores"])
@@ -399,7 +399,8 @@ def test_short_shards_whose_waves_share_a_block(k, dtype, fmt):
 
 @pytest.mark.parametrize("spec", [dict(B=48, Hq=8, Hkv=4, D=64, E=3, S=300, k=3), dict(B=47, Hq=8, Hkv=4, D=64, E=3, S=300, k=3),
                                   dict(B=100, Hq=2, Hkv=2, D=128, E=2, S=130, k=2, dtype="f32"), dict(B=25, Hq=8, Hkv=8, D=32, E=4, S=150, k=1, per_head=True),
-                                  dict(B=40, Hq=60, Hkv=5, D=64, E=2, S=90, k=2, tq=4, fmt=E4M3), dict(B=161, Hq=4, Hkv=4, D=32, E=2, S=33, k=1)],
+                                  dict(B=40, Hq=60, Hkv=5, D=64, E=2, S=90, k=2, tq=4, fmt=E4M3), dict(B=161, Hq=4, Hkv=4, D=32, E=2, S=33, k=1),
+                                  dict(B=96, Hq=32, Hkv=2, D=128, E=2, S=100, k=2), dict(B=99, Hq=32, Hkv=2, D=128, E=3, S=60, k=3, dtype="f32", fmt=E4M3)],
                          ids=lambda s: "B%d_Hkv%d_S%d" % (s["B"], s["Hkv"], s["S"]))
 def test_many_sequences(spec):
     """Enough (sequence, kv head) pairs for a block each, and one fewer."""
@@ -453,6 +454,48 @@ def test_a_poisoned_block_shows_in_the_rows_that_read_it_alone():
     a.run()
     torch.cuda.synchronize()
     assert torch.isfinite(a.y[0, :2]).all() and torch.isnan(a.y[0, 2:]).all()
+
+
+@pytest.mark.parametrize("S", [100, 700], ids=["merged", "split"])
+def test_a_poisoned_key_block_shows_too(S):
+    a = Attn(1, 4, 2, 64, 3, S, 2, n=S, seed=9, fmt=E4M3)
+    a.topk[:] = [[0, 1]]
+    a.buffers()
+    a.cache.scales[0][0, 1, 0, 1] = float("nan")        # kv head 0 of a selected shard
+    a.run()
+    torch.cuda.synchronize()
+    assert torch.isnan(a.y[0, :2]).all() and torch.isfinite(a.y[0, 2:]).all()
+
+
+@pytest.mark.parametrize("S", [100, 700], ids=["merged", "split"])
+def test_selections_of_no_shard_count_as_empty(S):
+    a = Attn(2, 8, 2, 64, 3, S, 3, seed=14)
+    a.topk[:] = [[2, 0, 1], [1, 2, 0]]
+    a.buffers()
+    a.d["topk"][0, 1], a.d["topk"][1, 2] = -1, 3
+    n = a.n.copy()
+    a.n[0, 0] = a.n[1, 0] = 0                            # the plain form: these shards are empty
+    a.run()
+    a.check()
+    a.n = n
+
+
+def test_a_shard_listed_twice_takes_a_new_entry_once():
+    caches = [Cache(1, 3, 2, 40, 64, "f32", INT8, 16) for _ in range(2)]
+    rng = np.random.default_rng(15)
+    values = make_values(rng, (1, 3, 2, 40, 64), "f32")
+    new = up(rng.normal(size=(1, 2, 64)) * 50)
+    counts = []
+    for cache, topk in zip(caches, ([[2, 0, 2]], [[2, 0, 1]])):
+        n, u = i32([[20, 20, 20]]), torch.ones((1, 3, 40), device=DEV)
+        cache.pack(values, n.cpu().numpy())
+        pk.pikv_quant_append(cache.desc, INT8, 16, new, new, i32(topk), 3, None, None, 0, *cache.tabs, *cache.scales, u, n)
+        torch.cuda.synchronize()
+        counts.append(n.tolist())
+    assert counts == [[[21, 20, 21]], [[21, 21, 21]]]
+    for a, b in zip(caches[0].codes + caches[0].scales, caches[1].codes + caches[1].scales):
+        a, b = a[0, [0, 2]], b[0, [0, 2]]
+        assert ((a == b) | (a != a)).all()
 
 
 def test_codes_behind_the_last_entry_and_their_scales_are_not_read():

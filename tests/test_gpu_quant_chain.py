@@ -126,6 +126,18 @@ def test_on_another_stream_than_the_current_one():
         assert all(torch.equal(u, v) for u, v in zip(a.state(), b.state()))
 
 
+def test_the_calls_through_ctypes_give_the_same_bits(monkeypatch):
+    a, b = Step(pk.QUANT_E4M3, seed=5), Step(pk.QUANT_E4M3, seed=5)
+    for x in a.steps[:3]:
+        a.x.copy_(x)
+        b.x.copy_(x)
+        a.calls()
+        with monkeypatch.context() as m:
+            m.setattr(pk.binding, "_native", pk.binding._NoExtension())
+            b.calls()
+        assert all(torch.equal(u, v) for u, v in zip(a.state(), b.state()))
+
+
 def test_two_captured_steps_replay_to_the_eager_bits():
     """Two graphs of two states, each with its own workspace, replayed in turn between eager steps of a third."""
     states, graphs = [Step(seed=2), Step(seed=3)], []
