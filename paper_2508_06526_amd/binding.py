@@ -530,10 +530,10 @@ def pikv_norm_rope(x, tokens, token_stride, Hq, Hkv, D, w_q, w_k, eps, positions
     """``x``: [tokens, heads * D] or [tokens, heads, D], rows ``token_stride`` elements apart (a view into a wider projection is
     taken as it is)."""
     where = "pikv_norm_rope"
-    _typed(where, x.dtype, w_q, w_k, q_out, k_out, v_out)
     st = _calls().pikv_norm_rope(x, tokens, token_stride, Hq, Hkv, D, w_q, w_k, eps, positions, inv_freq, rotary_dim,
                                  1 if interleaved else 0, q_out, k_out, v_out, _raw(stream))
     if st is None:
+        _typed(where, x.dtype, w_q, w_k, q_out, k_out, v_out)
         _int32_float32(where, [positions], [inv_freq])
         st = _on_device(where, lambda s: load_library().pikv_norm_rope(
             _rows(x, token_stride), tokens, token_stride, Hq, Hkv, D, _dtype_code(x), _p(w_q), _p(w_k), float(eps), _p(positions),
@@ -574,10 +574,10 @@ def pikv_quant_read(desc, format, block, K_shards, V_shards, K_scales, V_scales,
 def pikv_quant_append(desc, format, block, K_new, V_new, topk_idx, k, reuse_idx, reuse_cnt, max_evict, K_shards, V_shards, K_scales,
                       V_scales, utility, n_valid, stream=None):
     where = "pikv_quant_append"
-    _typed(where, _storage(desc), K_new, V_new)
     st = _calls().pikv_quant_append(desc, format, block, K_new, V_new, topk_idx, k, reuse_idx, reuse_cnt, max_evict, K_shards,
                                     V_shards, K_scales, V_scales, utility, n_valid, _raw(stream))
     if st is None:
+        _typed(where, _storage(desc), K_new, V_new)
         _int32_float32(where, [topk_idx, reuse_idx, reuse_cnt, n_valid], [K_scales, V_scales, utility], [K_shards, V_shards])
         st = _on_device(where, lambda s: load_library().pikv_quant_append(
             C.byref(desc), format, block, _p(K_new), _p(V_new), _p(topk_idx), k, _p(reuse_idx), _p(reuse_cnt), max_evict,
@@ -594,10 +594,10 @@ def pikv_quant_attn_workspace_bytes(desc: PikvDesc, k: int) -> int:
 def pikv_quant_attn(desc, format, block, q, K_shards, V_shards, K_scales, V_scales, n_valid, topk_idx, gates, k, combine, scale, y,
                     row_max, row_norm, scores, slot_coef, workspace, stream=None):
     where = "pikv_quant_attn"
-    _typed(where, _storage(desc), q)
     st = _calls().pikv_quant_attn(desc, format, block, q, K_shards, V_shards, K_scales, V_scales, n_valid, topk_idx, gates, k, combine,
                                   scale, y, row_max, row_norm, scores, slot_coef, workspace, _raw(stream))
     if st is None:
+        _typed(where, _storage(desc), q)
         _int32_float32(where, [n_valid, topk_idx], [K_scales, V_scales, gates, y, row_max, row_norm, scores, slot_coef],
                        [K_shards, V_shards])
         ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()

@@ -56,6 +56,7 @@ struct Args {
     const at::Tensor *last = nullptr;    // the last tensor taken
     const at::Tensor *first = nullptr;
     bool usual = true;                   // every argument so far was of the ordinary kind (no exception: one costs as much as a call)
+    at::ScalarType dense = at::ScalarType::Undefined;      // strict: the type of Dense tensors, the descriptor's or the first one's
     bool strict = false;                 // the tensors of int32_t *, float * and tables are of that type (tables: int64), and all are on one device
 
     template <typename T>
@@ -81,6 +82,7 @@ struct Args {
 struct Stream {};      // void *: the caller's, as an integer, or None - torch's current one
 struct Bytes {};       // size_t: of the tensor before it; takes no argument
 struct Dtype {};       // int32_t: of the first argument, a tensor; takes none itself
+struct Dense {};       // void *: a tensor of the descriptor's type, or of the first such tensor's
 struct DeviceStream {};      // void *: like Stream, torch's current one being that of the tensors' device; makes the call strict
 
 template <typename T, typename Kind>
@@ -88,7 +90,9 @@ struct Take {
     static T from(Args &a) {
         PyObject *o = *a.at++;
         if constexpr (std::is_same_v<T, const pikv_desc *>) {
-            return Py_TYPE(o) == desc_type ? a.template buffer<T>(o) : a.template unusual<T>();
+            T desc = Py_TYPE(o) == desc_type ? a.template buffer<T>(o) : a.template unusual<T>();
+            if (desc != nullptr) a.dense = desc->dtype == PIKV_F32 ? at::kFloat : at::kBFloat16;
+            return desc;
         } else if constexpr (std::is_same_v<T, const pikv_policy_args *> || std::is_same_v<T, const pikv_router_feedback *>) {
             if (o == Py_None) return nullptr;
             const bool mine = Py_TYPE(o) == (std::is_same_v<T, const pikv_policy_args *> ? policy_type : feedback_type);
@@ -137,6 +141,16 @@ struct Take<T, Stream> {
 };
 template <typename T>
 struct Take<T, DeviceStream> : Take<T, Stream> {};
+struct Plain {};
+template <typename T>
+struct Take<T, Dense> {
+    static T from(Args &a) {
+        T p = Take<T, Plain>::from(a);
+        if (p == nullptr) return nullptr;
+        if (a.dense == at::ScalarType::Undefined) a.dense = a.last->scalar_type();
+        return a.last->scalar_type() == a.dense ? p : a.template unusual<T>();
+    }
+};
 template <typename T>
 struct Take<T, Bytes> {
     static T from(Args &a) {
@@ -154,7 +168,6 @@ struct Take<T, Dtype> {
     }
 };
 
-struct Plain {};
 // The kind of parameter I: KINDS lists (index, kind) pairs for those that are not plain.
 template <int INDEX, typename KIND>
 struct At {};
@@ -246,11 +259,12 @@ PyMethodDef methods[] = {
     method<kPolicyUtility, decltype(&pikv_policy_utility), At<12, Stream>>("pikv_policy_utility"),
     method<kPolicyCompact, decltype(&pikv_policy_compact), At<8, Stream>>("pikv_policy_compact"),
     method<kPenalty, decltype(&pikv_router_penalty), At<9, Stream>>("pikv_router_penalty"),
-    method<kNormRope, decltype(&pikv_norm_rope), At<6, Dtype>, At<17, DeviceStream>>("pikv_norm_rope"),
+    method<kNormRope, decltype(&pikv_norm_rope), At<0, Dense>, At<6, Dtype>, At<7, Dense>, At<8, Dense>, At<14, Dense>, At<15, Dense>,
+           At<16, Dense>, At<17, DeviceStream>>("pikv_norm_rope"),
     method<kQuantPack, decltype(&pikv_quant_pack), At<12, DeviceStream>>("pikv_quant_pack"),
     method<kQuantRead, decltype(&pikv_quant_read), At<12, DeviceStream>>("pikv_quant_read"),
-    method<kQuantAppend, decltype(&pikv_quant_append), At<16, DeviceStream>>("pikv_quant_append"),
-    method<kQuantAttn, decltype(&pikv_quant_attn), At<20, Bytes>, At<21, DeviceStream>>("pikv_quant_attn"),
+    method<kQuantAppend, decltype(&pikv_quant_append), At<3, Dense>, At<4, Dense>, At<16, DeviceStream>>("pikv_quant_append"),
+    method<kQuantAttn, decltype(&pikv_quant_attn), At<3, Dense>, At<20, Bytes>, At<21, DeviceStream>>("pikv_quant_attn"),
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -522,6 +522,36 @@ def test_optional_outputs_do_not_change_the_others():
     assert torch.equal(a.y, y) and (a.scores == 7.0).all() and (a.row_max == 7.0).all()
 
 
+def test_device_tensors_of_another_kind_are_refused():
+    """By both paths of the binding, before anything is launched."""
+    a = Attn(1, 4, 2, 64, 3, 40, 2, seed=16)
+    c, d = a.cache, a.d
+    other, host = d["q"].float(), d["q"].cpu()
+    bf, i = torch.zeros(4096, device=DEV, dtype=torch.bfloat16), d["n"]
+    f = torch.zeros(4096, device=DEV)
+
+    def attn(q=d["q"], tab=c.tabs[0], n=d["n"], y=a.y):
+        pk.pikv_quant_attn(c.desc, c.fmt, c.block, q, tab, c.tabs[1], *c.scales, n, d["topk"], d["gates"], 2, pk.COMBINE_LSE, 0.0, y, None, None, None,
+                           None, a.ws)
+
+    def append(K_new=bf):
+        pk.pikv_quant_append(c.desc, c.fmt, c.block, K_new, bf, d["topk"], 2, None, None, 0, *c.tabs, *c.scales, f, d["n"])
+
+    def rope(w=bf, freq=f, positions=i):
+        pk.pikv_norm_rope(bf, 1, 512, 4, 2, 64, w, bf, 1e-6, positions, freq, 64, False, bf, bf, bf)
+
+    before = [t.clone() for t in c.codes + c.scales + [d["n"]]]
+    for call in (lambda: attn(q=other), lambda: attn(tab=c.codes[0]), lambda: attn(n=d["n"].long()), lambda: attn(y=a.y.double()), lambda: append(f),
+                 lambda: rope(w=f), lambda: rope(freq=f.double()), lambda: rope(positions=i.long())):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: attn(q=host), lambda: attn(tab=c.tabs[0].cpu()), lambda: attn(y=a.y.cpu()), lambda: attn(q=d["q"].transpose(1, 2))):
+        with pytest.raises(ValueError):
+            call()
+    torch.cuda.synchronize()
+    assert torch.isnan(a.y).all() and all(torch.equal(x.nan_to_num(), y.nan_to_num()) for x, y in zip(before, c.codes + c.scales + [d["n"]]))
+
+
 def test_no_sequences_is_a_no_op():
     d = pk.make_desc(0, 4, 4, 64, 2, 32, dtype=1)
     z, i, f = torch.zeros(64, device=DEV, dtype=torch.bfloat16), torch.zeros(4, device=DEV, dtype=torch.int32), torch.ones(64, device=DEV)
