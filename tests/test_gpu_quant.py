@@ -377,19 +377,20 @@ def test_draft_queries_in_the_tokens_layout(spec):
 
 
 @pytest.mark.parametrize("dtype,fmt", [("bf16", INT8), ("f32", E4M3)], ids=["bf16_int8", "f32_e4m3"])
-@pytest.mark.parametrize("k", range(1, 9))
+@pytest.mark.parametrize("k", [1, 2, 3, 4, 5, 6, 7, 8, 9, 16, 17])
 def test_short_shards_whose_waves_share_a_block(k, dtype, fmt):
-    """8 waves over k shards: 8, 4, 2 or 1 each, some left over; shards without entries, rows without any."""
-    n = np.random.default_rng(k).integers(0, 41, (3, 9)) * (np.random.default_rng(k + 50).random((3, 9)) < 0.7)
+    """8 waves over up to 8 shards: a power of two each, some left over; shards without entries, rows without any."""
+    E = max(9, k)
+    n = np.random.default_rng(k).integers(0, 41, (3, E)) * (np.random.default_rng(k + 50).random((3, E)) < 0.7)
     n[2] = 0
-    a = Attn(3, 12, 4, [128, 64][k % 2], 9, 40, k, dtype=dtype, fmt=fmt, block=16, n=n, seed=k, gates=k != 4)
+    a = Attn(3, 12, 4, [128, 64][k % 2], E, 40, k, dtype=dtype, fmt=fmt, block=16, n=n, seed=k, gates=k != 4)
     for combine in (pk.COMBINE_LSE, pk.COMBINE_LOCAL):
         a.run(combine)
         want = a.check(combine)
-        u = torch.rand((3, 9, 40), device=DEV)
+        u = torch.rand((3, E, 40), device=DEV)
         after = u.clone()
         pk.pikv_update_utility(a.cache.desc, a.scores, a.coef, a.d["n"], a.d["topk"], k, 0.5, after)
-        visited = np.zeros((3, 9, 1), bool)
+        visited = np.zeros((3, E, 1), bool)
         for b in range(3):
             visited[b, a.topk[b]] = True
         live = (np.arange(40) < n[..., None]) & visited
@@ -400,7 +401,8 @@ def test_short_shards_whose_waves_share_a_block(k, dtype, fmt):
 @pytest.mark.parametrize("spec", [dict(B=48, Hq=8, Hkv=4, D=64, E=3, S=300, k=3), dict(B=47, Hq=8, Hkv=4, D=64, E=3, S=300, k=3),
                                   dict(B=100, Hq=2, Hkv=2, D=128, E=2, S=130, k=2, dtype="f32"), dict(B=25, Hq=8, Hkv=8, D=32, E=4, S=150, k=1, per_head=True),
                                   dict(B=40, Hq=60, Hkv=5, D=64, E=2, S=90, k=2, tq=4, fmt=E4M3), dict(B=161, Hq=4, Hkv=4, D=32, E=2, S=33, k=1),
-                                  dict(B=96, Hq=32, Hkv=2, D=128, E=2, S=100, k=2), dict(B=99, Hq=32, Hkv=2, D=128, E=3, S=60, k=3, dtype="f32", fmt=E4M3)],
+                                  dict(B=96, Hq=32, Hkv=2, D=128, E=2, S=100, k=2), dict(B=99, Hq=32, Hkv=2, D=128, E=3, S=60, k=3, dtype="f32", fmt=E4M3),
+                                  dict(B=3, Hq=32, Hkv=2, D=128, E=2, S=200, k=2), dict(B=1, Hq=32, Hkv=2, D=64, E=20, S=40, k=16, dtype="f32")],
                          ids=lambda s: "B%d_Hkv%d_S%d" % (s["B"], s["Hkv"], s["S"]))
 def test_many_sequences(spec):
     """Enough (sequence, kv head) pairs for a block each, and one fewer."""
