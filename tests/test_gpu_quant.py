@@ -33,9 +33,9 @@ def i32(a):
 class Cache:
     """Shards of codes (bytes full of `fill`, scales NaN) with their dense side, rows `pad` elements apart beyond D."""
 
-    def __init__(self, B, E, Hkv, S, D, dtype, fmt, block, pad=0, gap=0, fill=0xA5, **desc):
+    def __init__(self, B, E, Hkv, S, D, dtype, fmt, block, pad=0, gap=0, fill=0xA5, dense_pad=None, **desc):
         self.shape, self.dtype, self.fmt, self.block = (B, E, Hkv, S, D), dtype, fmt, block
-        self.pad, self.rows = pad, S + gap
+        self.pad, self.rows = pad // 2 if dense_pad is None else dense_pad, S + gap
         self.codes = [torch.full((B, E, Hkv, self.rows, D + pad), fill, device=DEV, dtype=torch.uint8) for _ in range(2)]
         self.scales = [torch.full((B, E, Hkv, -(-S // block)), float("nan"), device=DEV) for _ in range(2)]
         self.tabs = [pk.shard_table([t[b, e] for b in range(B) for e in range(E)]) for t in self.codes]
@@ -45,7 +45,7 @@ class Cache:
     def dense(self, values=None):
         """Two dense shards (K, V) of the cache's type with their tables and strides."""
         B, E, Hkv, S, D = self.shape
-        pad = self.pad // 2
+        pad = self.pad
         bufs = [torch.full((B, E, Hkv, self.rows, D + pad), 3.0, device=DEV, dtype=DTYPES[self.dtype]) for _ in range(2)]
         if values is not None:
             for t, v in zip(bufs, values):
@@ -252,6 +252,32 @@ def test_append_into_a_block_of_zeros_that_was_never_written():
     pk.pikv_quant_append(cache.desc, E4M3, 16, rows, rows, i32([[0]]), 1, None, None, 0, *cache.tabs, *cache.scales, u, n)
     after = cache.read([[6]])
     assert all((t[0, 0, :, :5] == 0).all() and (t[0, 0, :, 5] != 0).any() for t in after)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows 4 MiB apart: a kv head's codes span 4.6 GiB, the second head starts behind them."""
+    B, E, Hkv, S, D, block = 1, 1, 2, 1150, 32, 64
+    cache = Cache(B, E, Hkv, S, D, "bf16", INT8, block, pad=(1 << 22) - D, dense_pad=0, Hq=4)
+    rng = np.random.default_rng(17)
+    values = make_values(rng, (B, E, Hkv, S, D), "bf16", spread=0.3)
+    n = i32([[S - 1]])
+    cache.pack(values, [[S - 1]])
+    new = [ref.rounded(rng.normal(size=(1, Hkv, D)) * 9, "bf16") for _ in range(2)]
+    u = torch.zeros((B, E, S), device=DEV)
+    pk.pikv_quant_append(cache.desc, INT8, block, up(new[0], "bf16"), up(new[1], "bf16"), i32([[0]]), 1, None, None, 0, *cache.tabs, *cache.scales, u, n)
+    check_read(cache, [[S]])
+    got, scales = cache.host()
+    want = expected_pack(values, np.array([[S - 1]]), INT8, block)
+    for g, s, (wc, ws), x in zip(got, scales, want, new):
+        ref.append(x[0].astype(np.float64), S - 1, S - 1, 0, INT8, block, wc[0, 0], ws[0, 0], S)
+        np.testing.assert_array_equal(s, ws.astype(np.float32))
+        same_codes(g, wc, INT8)
+    a = Attn(B, 4, Hkv, D, E, 8, 1)                      # (its geometry is replaced by the cache's)
+    a.geo, a.cache, a.n, a.topk, a.gates = (B, 4, Hkv, D, E, S, 1), cache, np.array([[S]]), np.array([[0]]), None
+    a.K, a.V = (ref.values(c, s, INT8, block) for c, s in zip(got, scales))
+    a.buffers()
+    a.run()
+    a.check()
 
 
 # ------------------------------------------------------------------------------ attention
