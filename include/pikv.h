@@ -406,7 +406,7 @@ int pikv_norm_rope(const void *x, int32_t tokens, int64_t token_stride, int32_t 
  *           and kv head, K and V apart.  Entry i of a row stands for code_i * scale.
  * Scales are powers of two (or 0 where nothing has been written: zeros): the smallest one, 2^-126 at
  * the least, that brings the largest magnitude of the block's rows within the largest code (127 or 448).
- * Divisions by it are then exact, a code is the nearest one (ties to even) to x / scale, and the value it
+ * Divisions by it are then exact, a code as it is written is the nearest one (ties to even) to x / scale, and the value it
  * stands for is exact in either dense type unless it underflows - every call here gives the same bits on
  * every machine.  A block that is given a NaN or an infinity has a NaN scale and reads as NaN until it is
  * written anew.
@@ -436,10 +436,12 @@ int pikv_quant_read(const pikv_desc *desc, int32_t format, int32_t block, const 
 
 /* pikv_append for these shards: the same slot rule, utility and count; the new rows [B,Hkv,D] dtype become
  * codes.  If other live slots share the block, its scale is the larger of its own and the one the new row
- * needs, and where that is larger than its own their codes are rounded to it; else (the block's first entry)
- * it is the new row's.  A scale does not shrink when the entry that set it leaves.  Live slots are those below
- * n_valid + 1 or, with reuse_cnt[b][e] = c > 1 freed slots, below n_valid + c; no other row's codes are
- * touched.  A shard listed twice in a row of topk_idx takes the entry once.
+ * needs, and where that is larger than its own their codes are rounded to it (a second time: what they stand for is
+ * then no longer the nearest code to what was given); else (the block's first entry) it is the new row's.  In a freed
+ * slot a scale comes down too: if the new row and the codes of the other live slots need an eighth of it or less, the
+ * block takes what they need, exactly, so that a large entry costs the block its precision no longer than it stays.
+ * Live slots are those below n_valid + 1 or, with reuse_cnt[b][e] = c > 1 freed slots, below n_valid + c; no other row's
+ * codes are touched.  A shard listed twice in a row of topk_idx takes the entry once.
  * Errors: descriptor errors, UNSUPPORTED as above and for B * k > 2^21, INVALID for null required pointers,
  * unknown format or block, k not in 1..E, one of reuse_idx and reuse_cnt without the other, max_evict < 1 with
  * them.  Per-token routing only (UNSUPPORTED otherwise).                                                  */

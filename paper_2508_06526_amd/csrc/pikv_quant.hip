@@ -165,9 +165,15 @@ struct QuantAppendParams {
     int E, S, Hkv, k, max_evict, n_blocks, block_bits;
 };
 
+// A scale that stands this far (exponents) above what its block needs comes down: at most four times the need is kept, six bits of
+// int8 at the least.  From eight times on, because the block's codes are read to find out and written again - the next entries
+// would mostly raise a closer scale again.
+constexpr uint32_t kMostSlack = 3u << 23, kOne = 127u << 23;
+
 // Two trips to memory, as append_rows: lane e takes shard e's count, freed slot and addresses beside the selection, which picks
-// among them, and the new rows come with those; then the block's old scale - and, where it grows, a third for its codes, eight
-// slots at a time.
+// among them, and the new rows come with those; then the block's old scale and the codes of the entry that leaves - and a third for
+// the block's codes, eight slots at a time, where the scale grows, or where the entry that leaves reaches within an eighth of it (else another
+// holds it up) and the new one does not.
 template <typename T, int D, int F>
 __global__ __launch_bounds__(1024) void quant_append(QuantAppendParams p) {
     constexpr int LPR = D / 8;
@@ -211,30 +217,53 @@ __global__ __launch_bounds__(1024) void quant_append(QuantAppendParams p) {
         float *at = (v ? p.V_scales : p.K_scales) + (be * p.Hkv + h) * p.n_blocks + blk;
         const uint32_t old = __float_as_uint(*at) & 0x7fffffffu;
         char *codes = (v ? Vs : Ks) + h * p.code_h + 8 * c;
+        uint2 leaves = make_uint2(0u, 0u);               // the lane's codes of the entry whose slot this is
+        if (cnt > 0) leaves = *reinterpret_cast<const uint2 *>(codes + (int64_t)slot * p.code_s);
         float f[8];
         x.widen(f);
         uint32_t scale = needed_scale<F>(lanes_max<LPR>(magnitude(f)));
-        if (others) scale = max(scale, old);
-        const float inv = inverse_scale(scale);
-        if (others && scale != old) {
-            // old / scale, at most 1/2; 0 from where it underflows, and codes with it (NaN scale: 0; so an old scale of 0, whose
-            // codes stand for zeros)
-            const int shift = (int)(scale >> 23) - (int)(old >> 23);
-            const float ratio = scale >= 0x7f800000u || old == 0 || shift > 126 ? 0.0f : __uint_as_float((uint32_t)(127 - shift) << 23);
+        // `use` with the lane's codes of each of the block's other live slots, eight requests together
+        auto for_others = [&](auto use) {
             constexpr int kAtOnce = 8;
             for (int s0 = lo; s0 < hi; s0 += kAtOnce) {
                 uint2 w[kAtOnce];
 #pragma unroll
                 for (int u = 0; u < kAtOnce; ++u) w[u] = *reinterpret_cast<const uint2 *>(codes + (int64_t)min(s0 + u, hi - 1) * p.code_s);
 #pragma unroll
-                for (int u = 0; u < kAtOnce; ++u) {
-                    float g[8];
-                    decode4<F>(w[u].x, g);
-                    decode4<F>(w[u].y, g + 4);
-                    const uint2 to = make_uint2(encode4<F>(g, ratio), encode4<F>(g + 4, ratio));
-                    if (s0 + u < hi && s0 + u != slot) *reinterpret_cast<uint2 *>(codes + (int64_t)(s0 + u) * p.code_s) = to;
-                }
+                for (int u = 0; u < kAtOnce; ++u)
+                    if (s0 + u < hi && s0 + u != slot) use(s0 + u, w[u]);
             }
+        };
+        auto largest = [&](uint2 w) {
+            float g[8];
+            decode4<F>(w.x, g);
+            decode4<F>(w.y, g + 4);
+            return magnitude(g);
+        };
+        if (others && scale + kMostSlack <= old && old < 0x7f800000u &&
+            needed_scale<F>(lanes_max<LPR>(largest(leaves))) + kMostSlack > kOne) {
+            // The entry that leaves may be what kept the scale up, and the new one needs far less: does what stays?
+            uint32_t most = 0;
+            for_others([&](int, uint2 w) { most = max(most, largest(w)); });
+            most = lanes_max<LPR>(most);
+            const int stays = most == 0 ? 0 : (int)(old >> 23) + (int)(needed_scale<F>(most) >> 23) - 127;     // biased exponent, may lie below the smallest
+            const uint32_t enough = max(scale, (uint32_t)max(stays, 1) << 23);
+            scale = enough + kMostSlack <= old ? enough : old;
+        } else if (others) {
+            scale = max(scale, old);
+        }
+        const float inv = inverse_scale(scale);
+        if (others && scale != old) {
+            // old / scale: at most 1/2, 0 from where it underflows, and codes with it (NaN scale: 0; so an old scale of 0, whose
+            // codes stand for zeros); or, of a scale that comes down, so large that no code saturates
+            const int shift = min((int)(old >> 23) - (int)(scale >> 23), 126);
+            const float ratio = scale >= 0x7f800000u || old == 0 || shift < -126 ? 0.0f : __uint_as_float((uint32_t)(127 + shift) << 23);
+            for_others([&](int s, uint2 w) {
+                float g[8];
+                decode4<F>(w.x, g);
+                decode4<F>(w.y, g + 4);
+                *reinterpret_cast<uint2 *>(codes + (int64_t)s * p.code_s) = make_uint2(encode4<F>(g, ratio), encode4<F>(g + 4, ratio));
+            });
         }
         *reinterpret_cast<uint2 *>(codes + (int64_t)slot * p.code_s) = make_uint2(encode4<F>(f, inv), encode4<F>(f + 4, inv));
         if (c == 0) *at = __uint_as_float(scale);

@@ -1,8 +1,8 @@
 // The 8-bit formats of the quantised cache: scales, codes and the values they stand for.
 //
-// A block's scale is a power of two, so x / scale is exact and a code is ONE rounding of x: kernels, tests and any other
-// machine agree to the bit, a value code * scale has at most 8 significant bits and is exact in bf16, and a block whose
-// scale grows rounds its codes by a shift of the exponent.  (With scale = max / 127 the midpoint max / 2 falls on a tie
+// A block's scale is a power of two, so x / scale is exact and a code as it is written is ONE rounding of x: kernels, tests and any
+// other machine agree to the bit, a value code * scale has at most 8 significant bits and is exact in bf16, and a block whose
+// scale grows rounds its codes (a second time) by a shift of the exponent.  (With scale = max / 127 the midpoint max / 2 falls on a tie
 // that fp32 decides by the error of its division; what a power of two costs is up to one bit of int8, none of e4m3.)
 #pragma once
 
