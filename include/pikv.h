@@ -404,12 +404,15 @@ int pikv_norm_rope(const void *x, int32_t tokens, int64_t token_stride, int32_t 
  *   format  pikv_quant_format; block: 16, 32, 64 or 128 slots that share a scale
  *   K_scales, V_scales [B,E,Hkv,ceil(S/block)] float32: one scale per block of slots
  *           and kv head, K and V apart.  Entry i of a row stands for code_i * scale.
- * Scales are powers of two (or 0 where nothing has been written: zeros): the smallest one, 2^-126 at
- * the least, that brings the largest magnitude of the block's rows within the largest code (127 or 448).
+ * Scales are powers of two (or 0 where nothing has been written: zeros): as pikv_quant_pack writes them, the smallest one,
+ * 2^-126 at the least, that brings the largest magnitude of the block's rows within the largest code (127 or 448).
  * Divisions by it are then exact, a code as it is written is the nearest one (ties to even) to x / scale, and the value it
  * stands for is exact in either dense type unless it underflows - every call here gives the same bits on
- * every machine.  A block that is given a NaN or an infinity has a NaN scale and reads as NaN until it is
- * written anew.
+ * every machine.  An entry with a NaN or an infinity has no codes, and the scale of its block is a NaN (its low bits
+ * keep the scale of the other entries' codes): the block reads as NaN until the slots of all such entries have
+ * been written anew, and then as if they had not been.  The exception is such an entry appended behind the last one, without a
+ * freed slot, to a block that holds others: the block then keeps no codes, later ones without a freed slot among
+ * them, and reads as NaN until all its slots have been written anew.
  * pikv_route, pikv_evict with compact == 0, pikv_policy_stamp, pikv_policy_utility and the utility updates
  * serve these shards as they are; pikv_evict with compact != 0 moves rows of the dense type and must not be
  * used on them, nor pikv_append, pikv_sharded_attn or the fused steps.                                   */

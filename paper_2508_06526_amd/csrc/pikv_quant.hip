@@ -10,7 +10,7 @@
 //   448), 1.6 GB in bf16 in 236 us (292; 237 - 257).  16-byte pieces of neighbouring lanes: with 8 fp32 values
 //   a lane, two pieces, half of every line was written at a time (127 MB 38 -> 26.7 us).
 //   quant_append : one block per (sequence, selected expert): slot rule and count of append_rows; a row of D values by D / 8
-//                  lanes, which also round the codes of the block's other live slots where its scale grows.
+//                  lanes, which also move the codes of the block's other live slots where its scale does.
 #include "pikv_mfma_dev.h"
 #include "pikv_quant_dev.h"
 
@@ -95,17 +95,37 @@ __global__ __launch_bounds__(WAVES *kWave) void quant_pack(QuantParams p) {
         Pack16<T>::widen(x[i], f);
         if (s0 + i * RPL + r < t.n) most = max(most, magnitude(f));
     }
-    most = lanes_max<kWave>(most);
-    if (lane == 0) wave_most[wave] = most;
-    __syncthreads();
-    const int together = 1 << (p.block_bits - 4);            // waves of a scale block: 1 .. 8
-    const int first = wave & ~(together - 1);
-    for (int w = 0; w < together; ++w) most = max(most, wave_most[first + w]);
+    const int together = 1 << (p.block_bits - 4), first = wave & ~(together - 1);            // waves of a scale block: 1 .. 8
+    auto of_scale_block = [&](uint32_t mine) {
+        mine = lanes_max<kWave>(mine);
+        if (lane == 0) wave_most[wave] = mine;
+        __syncthreads();
+        for (int w = 0; w < together; ++w) mine = max(mine, wave_most[first + w]);
+        return mine;
+    };
+    most = of_scale_block(most);
+    // A row with a NaN or an infinity has no codes, and no part in the scale.
+    const bool poisoned = most >= 0x7f800000u;
+    auto bad_row = [&](const float (&f)[VPL]) { return lanes_max<LPR>(magnitude(f)) >= 0x7f800000u; };
+    uint32_t of_block = 0;
+    for (int w = 0; w < WAVES; ++w) of_block = max(of_block, wave_most[w]);
+    if (of_block >= 0x7f800000u) {
+        __syncthreads();
+        uint32_t rest = 0;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            float f[VPL];
+            Pack16<T>::widen(x[i], f);
+            if (!bad_row(f) && s0 + i * RPL + r < t.n) rest = max(rest, magnitude(f));
+        }
+        most = of_scale_block(rest);
+    }
     if (s0 >= t.n) return;
     const uint32_t scale = needed_scale<F>(most);
     const float inv = inverse_scale(scale);
     if (lane == 0 && wave == first)
-        (t.v ? p.V_scales : p.K_scales)[((int64_t)t.be * p.Hkv + t.h) * p.n_blocks + (s0 >> p.block_bits)] = __uint_as_float(scale);
+        (t.v ? p.V_scales : p.K_scales)[((int64_t)t.be * p.Hkv + t.h) * p.n_blocks + (s0 >> p.block_bits)] =
+            __uint_as_float(poisoned ? poisoned_scale(scale) : scale);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
         const int slot = s0 + i * RPL + r;
@@ -114,6 +134,10 @@ __global__ __launch_bounds__(WAVES *kWave) void quant_pack(QuantParams p) {
         uint32_t w[VPL / 4];
 #pragma unroll
         for (int u = 0; u < VPL / 4; ++u) w[u] = encode4<F>(f + 4 * u, inv);
+        if (poisoned && bad_row(f)) {
+#pragma unroll
+            for (int u = 0; u < VPL / 4; ++u) w[u] = no_codes<F>();
+        }
         char *to = codes + (int64_t)slot * p.code_s;
         if (slot < t.n) {
             if constexpr (VPL == 4) *reinterpret_cast<uint32_t *>(to) = w[0];
@@ -168,7 +192,7 @@ struct QuantAppendParams {
 // A scale that stands this far (exponents) above what its block needs comes down: at most four times the need is kept, six bits of
 // int8 at the least.  From eight times on, because the block's codes are read to find out and written again - the next entries
 // would mostly raise a closer scale again.
-constexpr uint32_t kMostSlack = 3u << 23, kOne = 127u << 23;
+constexpr uint32_t kMostSlack = 3u << 23, kOne = 127u << 23, kLeastScale = 1u << 23;
 
 // Two trips to memory, as append_rows: lane e takes shard e's count, freed slot and addresses beside the selection, which picks
 // among them, and the new rows come with those; then the block's old scale and the codes of the entry that leaves - and a third for
@@ -215,13 +239,16 @@ __global__ __launch_bounds__(1024) void quant_append(QuantAppendParams p) {
         const int h = row >> 1, v = row & 1;
         if (row >= row_step) x = new_row(row);
         float *at = (v ? p.V_scales : p.K_scales) + (be * p.Hkv + h) * p.n_blocks + blk;
-        const uint32_t old = __float_as_uint(*at) & 0x7fffffffu;
+        const uint32_t word = __float_as_uint(*at) & 0x7fffffffu;
+        const bool poisoned = word >= 0x7f800000u;
+        const uint32_t old = poisoned ? kept_scale(word) : word;
         char *codes = (v ? Vs : Ks) + h * p.code_h + 8 * c;
         uint2 leaves = make_uint2(0u, 0u);               // the lane's codes of the entry whose slot this is
         if (cnt > 0) leaves = *reinterpret_cast<const uint2 *>(codes + (int64_t)slot * p.code_s);
         float f[8];
         x.widen(f);
-        uint32_t scale = needed_scale<F>(lanes_max<LPR>(magnitude(f)));
+        const uint32_t need = needed_scale<F>(lanes_max<LPR>(magnitude(f)));
+        const bool bad = need >= 0x7f800000u;
         // `use` with the lane's codes of each of the block's other live slots, eight requests together
         auto for_others = [&](auto use) {
             constexpr int kAtOnce = 8;
@@ -240,33 +267,53 @@ __global__ __launch_bounds__(1024) void quant_append(QuantAppendParams p) {
             decode4<F>(w.y, g + 4);
             return magnitude(g);
         };
-        if (others && scale + kMostSlack <= old && old < 0x7f800000u &&
-            needed_scale<F>(lanes_max<LPR>(largest(leaves))) + kMostSlack > kOne) {
-            // The entry that leaves may be what kept the scale up, and the new one needs far less: does what stays?
-            uint32_t most = 0;
-            for_others([&](int, uint2 w) { most = max(most, largest(w)); });
-            most = lanes_max<LPR>(most);
-            const int stays = most == 0 ? 0 : (int)(old >> 23) + (int)(needed_scale<F>(most) >> 23) - 127;     // biased exponent, may lie below the smallest
-            const uint32_t enough = max(scale, (uint32_t)max(stays, 1) << 23);
-            scale = enough + kMostSlack <= old ? enough : old;
-        } else if (others) {
-            scale = max(scale, old);
+        uint32_t scale;
+        bool marked = bad;                   // an entry of the block has no codes
+        if (!others) {
+            scale = need;
+        } else if (cnt <= 0 && (poisoned ? old == 0 : bad)) {
+            scale = kNanScale;               // without a freed slot: no codes are kept
+            if (!poisoned) for_others([&](int s, uint2) { *reinterpret_cast<uint2 *>(codes + (int64_t)s * p.code_s) = make_uint2(0u, 0u); });
+        } else if (poisoned && old == 0) {   // nothing was kept of the others: each is without codes until its slot is written
+            scale = bad ? kLeastScale : need;
+            marked = true;
+            for_others([&](int s, uint2) { *reinterpret_cast<uint2 *>(codes + (int64_t)s * p.code_s) = make_uint2(no_codes<F>(), no_codes<F>()); });
+        } else {
+            scale = bad ? max(old, kLeastScale) : max(need, old);
+            if (!bad && (poisoned || (need + kMostSlack <= old && needed_scale<F>(lanes_max<LPR>(largest(leaves))) + kMostSlack > kOne))) {
+                // The entry that leaves may be what kept the scale up, and the new one needs far less: does what stays?  Or it may have been
+                // the last one without codes.
+                uint32_t most = 0;
+                for_others([&](int, uint2 w) {
+                    if (poisoned && has_no_codes<F>(w.x)) marked = true;
+                    else most = max(most, largest(w));
+                });
+                most = lanes_max<LPR>(most);
+                const int stays = most == 0 ? 0 : (int)(old >> 23) + (int)(needed_scale<F>(most) >> 23) - 127;     // biased exponent, may lie below the smallest
+                const uint32_t enough = max(need, (uint32_t)max(stays, 1) << 23);
+                if (cnt > 0 && enough + kMostSlack <= scale) scale = enough;
+            }
+            if (scale != old) {
+                // old / scale: at most 1/2, 0 from where it underflows, and codes with it (so an old scale of 0, whose codes stand for
+                // zeros); or, of a scale that comes down, so large that no code saturates
+                const int shift = min((int)(old >> 23) - (int)(scale >> 23), 126);
+                const float ratio = old == 0 || shift < -126 ? 0.0f : __uint_as_float((uint32_t)(127 + shift) << 23);
+                for_others([&](int s, uint2 w) {
+                    if (poisoned && has_no_codes<F>(w.x)) return;
+                    float g[8];
+                    decode4<F>(w.x, g);
+                    decode4<F>(w.y, g + 4);
+                    *reinterpret_cast<uint2 *>(codes + (int64_t)s * p.code_s) = make_uint2(encode4<F>(g, ratio), encode4<F>(g + 4, ratio));
+                });
+            }
         }
-        const float inv = inverse_scale(scale);
-        if (others && scale != old) {
-            // old / scale: at most 1/2, 0 from where it underflows, and codes with it (NaN scale: 0; so an old scale of 0, whose
-            // codes stand for zeros); or, of a scale that comes down, so large that no code saturates
-            const int shift = min((int)(old >> 23) - (int)(scale >> 23), 126);
-            const float ratio = scale >= 0x7f800000u || old == 0 || shift < -126 ? 0.0f : __uint_as_float((uint32_t)(127 + shift) << 23);
-            for_others([&](int s, uint2 w) {
-                float g[8];
-                decode4<F>(w.x, g);
-                decode4<F>(w.y, g + 4);
-                *reinterpret_cast<uint2 *>(codes + (int64_t)s * p.code_s) = make_uint2(encode4<F>(g, ratio), encode4<F>(g + 4, ratio));
-            });
+        uint2 to = make_uint2(0u, 0u);
+        if (scale < 0x7f800000u) {
+            const float inv = inverse_scale(scale);
+            to = bad ? make_uint2(no_codes<F>(), no_codes<F>()) : make_uint2(encode4<F>(f, inv), encode4<F>(f + 4, inv));
         }
-        *reinterpret_cast<uint2 *>(codes + (int64_t)slot * p.code_s) = make_uint2(encode4<F>(f, inv), encode4<F>(f + 4, inv));
-        if (c == 0) *at = __uint_as_float(scale);
+        *reinterpret_cast<uint2 *>(codes + (int64_t)slot * p.code_s) = to;
+        if (c == 0) *at = __uint_as_float(scale < 0x7f800000u && marked ? poisoned_scale(scale) : scale);
     }
     if (tid == 0) {
         p.utility[be * p.S + slot] = 0.0f;

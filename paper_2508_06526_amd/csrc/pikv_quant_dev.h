@@ -25,6 +25,20 @@ inline int check_quant(const pikv_desc *d, int format, int block) {
 // that of the scales, a NaN above all.
 constexpr uint32_t kNanScale = 0x7fc00000u;
 
+// A block with an entry that holds a NaN or an infinity has a NaN for a scale, whose low eight bits are the exponent of the scale
+// that the other entries' codes have, and that entry, in place of codes, a byte that no finite value gets: all read as
+// NaN until such entries are gone, the others as before from then on.  Exponent 0: no codes were kept.
+__device__ __forceinline__ uint32_t poisoned_scale(uint32_t scale) { return kNanScale | scale >> 23; }
+__device__ __forceinline__ uint32_t kept_scale(uint32_t word) { return (word & ~0xffu) == kNanScale ? (word & 0xffu) << 23 : 0u; }
+template <int F>
+__device__ __forceinline__ uint32_t no_codes() {
+    return F == PIKV_QUANT_INT8 ? 0x80808080u : 0x7f7f7f7fu;
+}
+template <int F>
+__device__ __forceinline__ bool has_no_codes(uint32_t codes) {
+    return F == PIKV_QUANT_INT8 ? (codes & 0xffu) == 0x80u : (codes & 0x7fu) == 0x7fu;
+}
+
 // The scale needed by magnitudes of up to `most` (bits of a non-negative fp32): the smallest power of two, 2^-126 at
 // the least, with most <= limit * scale, limit = 127 = 1.984375 * 2^6 or 448 = 1.75 * 2^8.
 template <int F>

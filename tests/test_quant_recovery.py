@@ -70,3 +70,44 @@ def test_a_stream_recovers_from_one_large_entry(fmt):
         assert (np.abs(got[hold] - held[hold]) <= step).all()
     worst = stream(ref.append, fmt, S, block, D, order, rows, rng.normal(size=(S, D)))[1]
     assert worst[0, 1] >= 64 * scales[0, 1]                          # (the scale of the large entry, had it stayed)
+
+
+def word(scales):
+    return int(rec.bits(scales)[0, 0])
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_a_row_that_is_not_finite_leaves_the_others_their_codes(bad):
+    codes, scales = block_of([[100.0, 3.0], [7.0, 1.0], [-2.0, 5.0]], 0)
+    assert scales[0, 0] == 1.0
+    rec.append(np.array([[bad, 1.0]]), 1, 2, 1, 0, 16, codes, scales, 3)
+    assert word(scales) == 0x7fc0007f and codes.view(np.int8)[0].tolist() == [[100, 3], [-128, -128], [-2, 5]]
+    rec.append(np.array([[200.0, 1.0]]), 2, 2, 1, 0, 16, codes, scales, 3)      # its neighbour's scale grows meanwhile
+    assert word(scales) == 0x7fc00080 and codes.view(np.int8)[0].tolist() == [[50, 2], [-128, -128], [100, 0]]
+    rec.append(np.array([[4.0, 3.0]]), 1, 2, 1, 0, 16, codes, scales, 3)
+    assert scales[0, 0] == 2.0 and codes.view(np.int8)[0].tolist() == [[50, 2], [2, 2], [100, 0]]
+
+
+def test_a_block_that_kept_nothing_is_whole_again_once_every_slot_is_rewritten():
+    codes, scales = block_of([[1.0, 2.0], [3.0, 4.0], [5.0, 6.0]], 1)
+    rec.append(np.array([[np.nan, 0.0]]), 2, 2, 0, 1, 16, codes, scales, 3)     # behind the last entry: no freed slot
+    assert np.isnan(scales[0, 0]) and (codes == 0).all()
+    for slot in (0, 2, 1):
+        assert np.isnan(scales[0, 0])
+        rec.append(np.array([[448.0, slot + 1.0]]), slot, 2, 1, 1, 16, codes, scales, 3)
+    assert (ref.decode(codes, 1) * scales[0, 0] == [[[448, 1], [448, 2], [448, 3]]]).all()
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_packed_rows_that_are_not_finite_have_no_part_in_the_scale(fmt):
+    rng = np.random.default_rng(1)
+    clean = rng.normal(size=(1, 1, 1, 40, 32))
+    dirty = clean.copy()
+    dirty[0, 0, 0, [3, 5, 35], [0, 31, 7]] = [np.nan, np.inf, -np.inf]
+    out = [(np.full(clean.shape, 9, np.uint8), np.zeros((1, 1, 1, 3), np.float32)) for _ in range(2)]
+    for x, (c, s) in zip((np.where(np.isfinite(dirty).all(-1, keepdims=True), clean, 0), dirty), out):
+        rec.pack(x, np.array([[38]]), fmt, 16, c, s)
+    (want, ws), (got, gs) = out
+    rows = np.isin(np.arange(40), [3, 5, 35])
+    assert (got[0, 0, 0, ~rows] == want[0, 0, 0, ~rows]).all() and (got[0, 0, 0, rows] == rec.NO_CODES[fmt]).all()
+    assert [rec.kept(w) for w in rec.bits(gs)[0, 0, 0]] == ws[0, 0, 0].tolist() and np.isnan(gs[0, 0, 0]).tolist() == [True, False, True]
