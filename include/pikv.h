@@ -69,7 +69,7 @@ typedef struct pikv_desc {
     int64_t stride_h; /* elements between kv heads inside a shard buffer                   */
     int64_t stride_s; /* elements between slots (>= width, multiple of 16 bytes)           */
     int32_t route_rows_per_seq; /* 1 or Hq                                                 */
-    int32_t flags;    /* 0, or PIKV_DESC_VALUE_BIAS (rank > 0 only)                        */
+    int32_t flags;    /* 0, PIKV_DESC_VALUE_BIAS (rank > 0 only) or PIKV_DESC_8BIT (rank 0) */
     int32_t tq;       /* draft queries per sequence in a multi-query step; 0 or 1: one query */
     int32_t reserved; /* must be 0                                                         */
 } pikv_desc;
@@ -94,6 +94,10 @@ typedef struct pikv_desc {
  * row with a non-empty selection - gains b[h'].  (The same term on the key side would shift all
  * scores of a head equally and cancel in the softmax, so U_K never carries one.)             */
 #define PIKV_DESC_VALUE_BIAS 1
+/* PIKV_DESC_8BIT: the shards hold codes of one byte ("The cache held in 8 bits" below; strides count bytes).  The calls
+ * that would read or write rows of the dense type refuse such a descriptor (INVALID); the calls on 8-bit shards take
+ * one without the flag as well.                                                                              */
+#define PIKV_DESC_8BIT 2
 
 /* Section 3.2, Table 1 "TopK softmax" router (with the table's additive per-expert
  * penalty as `bias`): logits = x W_r + bias, p = softmax over the E experts, the mask has
@@ -413,9 +417,10 @@ int pikv_norm_rope(const void *x, int32_t tokens, int64_t token_stride, int32_t 
  * been written anew, and then as if they had not been.  The exception is such an entry appended behind the last one, without a
  * freed slot, to a block that holds others: the block then keeps no codes, later ones without a freed slot among
  * them, and reads as NaN until all its slots have been written anew.
- * pikv_route, pikv_evict with compact == 0, pikv_policy_stamp, pikv_policy_utility and the utility updates
- * serve these shards as they are; pikv_evict with compact != 0 moves rows of the dense type and must not be
- * used on them, nor pikv_append, pikv_sharded_attn or the fused steps.                                   */
+ * pikv_route, pikv_evict with compact == 0, the pikv_policy calls and the utility updates serve these shards as
+ * they are.  pikv_evict with compact != 0, pikv_append, pikv_sharded_attn and the fused steps work on rows of the
+ * dense type and must not be used on them: they would write behind the shards.  Set PIKV_DESC_8BIT in the
+ * descriptor of such a cache, and they refuse it.                                                           */
 typedef enum { PIKV_QUANT_INT8 = 0, PIKV_QUANT_E4M3 = 1 } pikv_quant_format;
 
 /* Writes shards from dense ones: codes of the entries 0 .. n_valid[b][e]-1 (at most S) and the scales of the

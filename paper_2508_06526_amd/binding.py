@@ -23,7 +23,7 @@ _NATIVE_PATH = os.path.join(_HERE, "_pikv_native.so")
 F32, BF16 = 0, 1
 COMBINE_LSE, COMBINE_LOCAL = 0, 1
 PENALTY_LOAD_BALANCE, PENALTY_CACHE_AWARE, PENALTY_ENTROPY = 0, 1, 2
-DESC_VALUE_BIAS = 1
+DESC_VALUE_BIAS, DESC_8BIT = 1, 2
 POLICY_H2O, POLICY_SL, POLICY_LRU, POLICY_LRU_PLUS = 0, 1, 2, 3
 QUANT_INT8, QUANT_E4M3 = 0, 1
 
@@ -165,7 +165,7 @@ def _load_native(addresses):
         warnings.warn("calls go through ctypes: _pikv_native.so is not built for this Python and torch (%s); "
                       "run `python -m paper_2508_06526_amd.build`" % e, RuntimeWarning, stacklevel=3)
         return _NoExtension()
-    native.setup(PikvDesc, PikvPolicyArgs, PikvRouterFeedback, addresses)
+    native.setup(PikvDesc, PikvPolicyArgs, PikvRouterFeedback, addresses, _MARK)
     return native
 
 
@@ -237,7 +237,9 @@ def make_desc(B, Hq, Hkv, D, E, S, rank=0, dtype=BF16, stride_h=None, stride_s=N
 def shard_table(shards, device=None):
     """Device array of B*E shard base addresses (entry b*E+e).
 
-    ``shards`` is a tensor [B,E,Hkv,S,w] (one allocation) or a flat list of B*E tensors.
+    ``shards`` is a tensor [B,E,Hkv,S,w] (one allocation) or a flat list of B*E tensors.  A table of int8 or float8_e4m3fn
+    shards is marked as one: the calls on rows of the dense type, which would write behind such shards, refuse it (of
+    shards of other types - raw bytes among them - nothing is known; PIKV_DESC_8BIT in the descriptor tells).
     """
     import torch
     if isinstance(shards, torch.Tensor):
@@ -249,7 +251,20 @@ def shard_table(shards, device=None):
     else:
         ptrs = [s.data_ptr() for s in shards]
         device = shards[0].device
-    return torch.tensor(ptrs, dtype=torch.int64, device=device)
+    table = torch.tensor(ptrs, dtype=torch.int64, device=device)
+    if (shards if isinstance(shards, torch.Tensor) else shards[0]).dtype in (torch.int8, torch.float8_e4m3fn):
+        setattr(table, _MARK, True)
+    return table
+
+
+_MARK = "_pikv_8bit"         # attribute of a table of 8-bit shards
+
+
+def _dense(where, *tables):
+    """Tables of shards of the dense type."""
+    for t in tables:
+        if getattr(t, _MARK, False):
+            raise TypeError("%s: works on rows of the dense type, the table is of 8-bit shards" % where)
 
 
 def pikv_strerror(status: int) -> str:
@@ -289,6 +304,7 @@ def pikv_sharded_attn(desc, q, K_shards, V_shards, U_K, U_V, n_valid, topk_idx, 
     st = _calls().pikv_sharded_attn(desc, q, K_shards, V_shards, U_K, U_V, n_valid, topk_idx, gates, k, combine, scale, y,
                                     row_max, row_norm, scores, slot_coef, workspace, _raw(stream))
     if st is None:
+        _dense("pikv_sharded_attn", K_shards, V_shards)
         ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
         st = load_library().pikv_sharded_attn(
             C.byref(desc), _p(q), _p(K_shards), _p(V_shards), _p(U_K), _p(U_V), _p(n_valid),
@@ -306,6 +322,7 @@ def pikv_sharded_attn_noalloc(desc, q, K_shards, V_shards, U_K, U_V, n_valid, to
     st = _calls().pikv_sharded_attn_noalloc(desc, q, K_shards, V_shards, U_K, U_V, n_valid, topk_idx, gates, k, combine, scale,
                                             y, row_max, row_norm, scores, slot_coef, _raw(stream))
     if st is None:
+        _dense("pikv_sharded_attn_noalloc", K_shards, V_shards)
         st = load_library().pikv_sharded_attn_noalloc(
             C.byref(desc), _p(q), _p(K_shards), _p(V_shards), _p(U_K), _p(U_V), _p(n_valid),
             _p(topk_idx), _p(gates), k, combine, float(scale), _p(y), _p(row_max), _p(row_norm),
@@ -329,6 +346,8 @@ def pikv_evict(desc, utility, n_valid, capacity, sel_idx, sel_k, evicted_idx, ev
     st = _calls().pikv_evict(desc, utility, n_valid, capacity, sel_idx, sel_k, evicted_idx, evicted_cnt, max_evict,
                              1 if compact else 0, K_shards, V_shards, _raw(stream))
     if st is None:
+        if compact:
+            _dense("pikv_evict", K_shards, V_shards)
         st = load_library().pikv_evict(C.byref(desc), _p(utility), _p(n_valid), capacity, _p(sel_idx),
                                        sel_k, _p(evicted_idx), _p(evicted_cnt), max_evict,
                                        1 if compact else 0, _p(K_shards), _p(V_shards), _stream(stream))
@@ -341,6 +360,7 @@ def pikv_append(desc, K_new, V_new, topk_idx, k, reuse_idx, reuse_cnt, max_evict
     st = _calls().pikv_append(desc, K_new, V_new, topk_idx, k, reuse_idx, reuse_cnt, max_evict, K_shards, V_shards,
                               utility, n_valid, _raw(stream))
     if st is None:
+        _dense("pikv_append", K_shards, V_shards)
         st = load_library().pikv_append(C.byref(desc), _p(K_new), _p(V_new), _p(topk_idx), k,
                                         _p(reuse_idx), _p(reuse_cnt), max_evict, _p(K_shards),
                                         _p(V_shards), _p(utility), _p(n_valid), _stream(stream))
@@ -355,6 +375,7 @@ def pikv_decode_step(desc, q, W_r, bias, K_new, V_new, K_shards, V_shards, U_K, 
                                    combine, scale, decay, topk_idx, gates, evicted_idx, evicted_cnt, y, row_max,
                                    row_norm, scores, slot_coef, workspace, _raw(stream))
     if st is None:
+        _dense("pikv_decode_step", K_shards, V_shards)
         ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
         st = load_library().pikv_decode_step(
             C.byref(desc), _p(q), _p(W_r), _p(bias), _p(K_new), _p(V_new), _p(K_shards), _p(V_shards),
@@ -462,6 +483,7 @@ def pikv_decode_step_policy(desc, q, W_r, bias, K_new, V_new, K_shards, V_shards
                                           combine, scale, decay, topk_idx, gates, evicted_idx, evicted_cnt, y, row_max,
                                           row_norm, scores, slot_coef, workspace, _raw(stream), policy_args, feedback)
     if st is None:
+        _dense("pikv_decode_step_policy", K_shards, V_shards)
         st = load_library().pikv_decode_step_policy(
             C.byref(desc), _p(q), _p(W_r), _p(bias), _p(K_new), _p(V_new), _p(K_shards), _p(V_shards), _p(U_K),
             _p(U_V), _p(n_valid), _p(utility), k, combine, float(scale), float(decay), _p(topk_idx), _p(gates),
@@ -549,6 +571,7 @@ def pikv_quant_pack(desc, format, block, K_dense, V_dense, dense_stride_h, dense
     st = _calls().pikv_quant_pack(desc, format, block, K_dense, V_dense, dense_stride_h, dense_stride_s, n_valid, K_shards, V_shards,
                                   K_scales, V_scales, _raw(stream))
     if st is None:
+        _dense(where, K_dense, V_dense)
         _int32_float32(where, [n_valid], [K_scales, V_scales], [K_dense, V_dense, K_shards, V_shards])
         st = _on_device(where, lambda s: load_library().pikv_quant_pack(
             C.byref(desc), format, block, _p(K_dense), _p(V_dense), dense_stride_h, dense_stride_s, _p(n_valid), _p(K_shards),
@@ -563,6 +586,7 @@ def pikv_quant_read(desc, format, block, K_shards, V_shards, K_scales, V_scales,
     st = _calls().pikv_quant_read(desc, format, block, K_shards, V_shards, K_scales, V_scales, n_valid, K_dense, V_dense,
                                   dense_stride_h, dense_stride_s, _raw(stream))
     if st is None:
+        _dense(where, K_dense, V_dense)
         _int32_float32(where, [n_valid], [K_scales, V_scales], [K_dense, V_dense, K_shards, V_shards])
         st = _on_device(where, lambda s: load_library().pikv_quant_read(
             C.byref(desc), format, block, _p(K_shards), _p(V_shards), _p(K_scales), _p(V_scales), _p(n_valid), _p(K_dense),

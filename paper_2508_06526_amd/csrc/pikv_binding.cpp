@@ -26,6 +26,13 @@ namespace {
 // The classes of binding.py's ctypes structures; set once by setup(), which the binding calls when it loads the library.
 PyTypeObject *desc_type = nullptr, *policy_type = nullptr, *feedback_type = nullptr;
 
+// What shard_table marks tables of 8-bit shards with: only the calls on such shards take them.
+PyObject *eight_bit_mark = nullptr;
+bool of_eight_bits(PyObject *tensor) {
+    PyObject **attributes = _PyObject_GetDictPtr(tensor);
+    return attributes != nullptr && *attributes != nullptr && PyDict_Contains(*attributes, eight_bit_mark) == 1;
+}
+
 // Addresses of the library's functions, in the order of `Functions`.
 enum Function {
     kRoute, kAttn, kAttnNoalloc, kUtility, kUtilityTracked, kEvict, kAppend, kStep, kStepPolicy, kCompress, kStamp, kPolicyUtility,
@@ -83,6 +90,7 @@ struct Stream {};      // void *: the caller's, as an integer, or None - torch's
 struct Bytes {};       // size_t: of the tensor before it; takes no argument
 struct Dtype {};       // int32_t: of the first argument, a tensor; takes none itself
 struct Dense {};       // void *: a tensor of the descriptor's type, or of the first such tensor's
+struct Codes {};       // void *const *: a table of 8-bit shards; one that is not Codes is of shards of the dense type
 struct DeviceStream {};      // void *: like Stream, torch's current one being that of the tensors' device; makes the call strict
 
 template <typename T, typename Kind>
@@ -104,6 +112,8 @@ struct Take {
                                              (std::is_same_v<Element, float> && t->scalar_type() != at::kFloat) ||
                                              (std::is_pointer_v<Element> && t->scalar_type() != at::kLong)))
                 return a.template unusual<T>();
+            if constexpr (std::is_pointer_v<Element> && !std::is_same_v<Kind, Codes>)
+                if (t != nullptr && of_eight_bits(o)) return a.template unusual<T>();
             a.last = t;
             if (a.first == nullptr) a.first = t;
             return t == nullptr ? nullptr : static_cast<T>(t->data_ptr());
@@ -240,7 +250,7 @@ PyMethodDef method(const char *name) {
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&Caller<F, FN, KINDS...>::call)), METH_FASTCALL, nullptr};
 }
 
-// setup(descriptor class, policy class, feedback class, {name: address})
+// setup(descriptor class, policy class, feedback class, {name: address}, attribute of tables of 8-bit shards)
 PyObject *setup(PyObject *, PyObject *args);
 
 PyMethodDef methods[] = {
@@ -261,17 +271,21 @@ PyMethodDef methods[] = {
     method<kPenalty, decltype(&pikv_router_penalty), At<9, Stream>>("pikv_router_penalty"),
     method<kNormRope, decltype(&pikv_norm_rope), At<0, Dense>, At<6, Dtype>, At<7, Dense>, At<8, Dense>, At<14, Dense>, At<15, Dense>,
            At<16, Dense>, At<17, DeviceStream>>("pikv_norm_rope"),
-    method<kQuantPack, decltype(&pikv_quant_pack), At<12, DeviceStream>>("pikv_quant_pack"),
-    method<kQuantRead, decltype(&pikv_quant_read), At<12, DeviceStream>>("pikv_quant_read"),
-    method<kQuantAppend, decltype(&pikv_quant_append), At<3, Dense>, At<4, Dense>, At<16, DeviceStream>>("pikv_quant_append"),
-    method<kQuantAttn, decltype(&pikv_quant_attn), At<3, Dense>, At<20, Bytes>, At<21, DeviceStream>>("pikv_quant_attn"),
+    method<kQuantPack, decltype(&pikv_quant_pack), At<8, Codes>, At<9, Codes>, At<12, DeviceStream>>("pikv_quant_pack"),
+    method<kQuantRead, decltype(&pikv_quant_read), At<3, Codes>, At<4, Codes>, At<12, DeviceStream>>("pikv_quant_read"),
+    method<kQuantAppend, decltype(&pikv_quant_append), At<3, Dense>, At<4, Dense>, At<10, Codes>, At<11, Codes>, At<16, DeviceStream>>(
+        "pikv_quant_append"),
+    method<kQuantAttn, decltype(&pikv_quant_attn), At<3, Dense>, At<4, Codes>, At<5, Codes>, At<20, Bytes>, At<21, DeviceStream>>(
+        "pikv_quant_attn"),
     {nullptr, nullptr, 0, nullptr},
 };
 
 PyObject *setup(PyObject *, PyObject *args) {
     PyObject *desc, *policy, *feedback, *table;
-    if (!PyArg_ParseTuple(args, "O!O!O!O!", &PyType_Type, &desc, &PyType_Type, &policy, &PyType_Type, &feedback, &PyDict_Type, &table))
+    const char *mark;
+    if (!PyArg_ParseTuple(args, "O!O!O!O!s", &PyType_Type, &desc, &PyType_Type, &policy, &PyType_Type, &feedback, &PyDict_Type, &table, &mark))
         return nullptr;
+    if ((eight_bit_mark = PyUnicode_InternFromString(mark)) == nullptr) return nullptr;
     for (int f = 0; f < kFunctions; ++f) {
         PyObject *address = PyDict_GetItemString(table, methods[f + 1].ml_name);
         if (address == nullptr) return PyErr_Format(PyExc_KeyError, "%s", methods[f + 1].ml_name);

@@ -222,8 +222,9 @@ inline hipStream_t as_stream(void *s) { return reinterpret_cast<hipStream_t>(s);
 
 inline int launch_status() { return hipGetLastError() == hipSuccess ? PIKV_OK : PIKV_ERR_HIP; }
 
-// Host-side descriptor checks common to every call that takes a pikv_desc.
-int check_desc(const pikv_desc *d);
+// Host-side descriptor checks common to every call that takes a pikv_desc.  A call that reads or writes rows of the dense type refuses the
+// descriptor of an 8-bit cache; `eight_bit`: the call serves that too.
+int check_desc(const pikv_desc *d, bool eight_bit = false);
 inline int desc_width(const pikv_desc *d) { return d->rank ? d->rank : d->D; }
 inline int elem_bytes(int dtype) { return dtype == PIKV_F32 ? 4 : 2; }
 

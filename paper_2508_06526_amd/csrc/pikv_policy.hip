@@ -112,7 +112,7 @@ extern "C" int pikv_policy_compact(const pikv_desc *desc, const int32_t *evicted
                                    const int32_t *evicted_cnt, int32_t max_evict,
                                    const int32_t *n_valid, int32_t *birth, int32_t *last_access,
                                    int32_t *freq, void *stream) {
-    const int rc = check_desc(desc);
+    const int rc = check_desc(desc, true);
     if (rc != PIKV_OK) return rc;
     if (!evicted_idx || !evicted_cnt || !n_valid || !birth || !last_access || !freq)
         return PIKV_ERR_INVALID;
@@ -137,7 +137,7 @@ extern "C" int pikv_policy_stamp(const pikv_desc *desc, const int32_t *topk_idx,
                                  int32_t max_evict, const int32_t *n_valid, int32_t now,
                                  int32_t *birth, int32_t *last_access, int32_t *freq,
                                  void *stream) {
-    const int rc = check_desc(desc);
+    const int rc = check_desc(desc, true);
     if (rc != PIKV_OK) return rc;
     if (!topk_idx || !n_valid || !birth || !last_access || !freq) return PIKV_ERR_INVALID;
     if (k < 1 || k > desc->E) return PIKV_ERR_INVALID;
@@ -169,7 +169,7 @@ extern "C" int pikv_policy_utility(const pikv_desc *desc, int32_t policy, const 
                                    const int32_t *birth, const int32_t *last_access,
                                    const int32_t *freq, const float *h2o, float *out,
                                    void *stream) {
-    const int rc = check_desc(desc);
+    const int rc = check_desc(desc, true);
     if (rc != PIKV_OK) return rc;
     if (!n_valid || !out) return PIKV_ERR_INVALID;
     const int prc = check_policy(policy, window, protect, lambda, birth, last_access, freq, h2o);

@@ -12,7 +12,7 @@ namespace pikv {
 
 // Host-side checks common to the calls on 8-bit shards.
 inline int check_quant(const pikv_desc *d, int format, int block) {
-    const int rc = check_desc(d);
+    const int rc = check_desc(d, true);
     if (rc != PIKV_OK) return rc;
     if (format != PIKV_QUANT_INT8 && format != PIKV_QUANT_E4M3) return PIKV_ERR_INVALID;
     if (block != 16 && block != 32 && block != 64 && block != 128) return PIKV_ERR_INVALID;

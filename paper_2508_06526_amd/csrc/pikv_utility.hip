@@ -270,7 +270,7 @@ extern "C" int pikv_update_utility(const pikv_desc *desc, const float *scores,
                                    const float *slot_coef, const int32_t *n_valid,
                                    const int32_t *topk_idx, int32_t k, float decay,
                                    float *utility, void *stream) {
-    const int rc = check_desc(desc);
+    const int rc = check_desc(desc, true);
     if (rc != PIKV_OK) return rc;
     if (!scores || !slot_coef || !n_valid || !topk_idx || !utility) return PIKV_ERR_INVALID;
     if (k < 1 || k > desc->E) return PIKV_ERR_INVALID;
@@ -285,7 +285,7 @@ extern "C" int pikv_update_utility_tracked(const pikv_desc *desc, const float *s
                                            const int32_t *topk_idx, int32_t k, float decay,
                                            float *utility, float threshold, int32_t now,
                                            int32_t *last_access, int32_t *freq, void *stream) {
-    const int rc = check_desc(desc);
+    const int rc = check_desc(desc, true);
     if (rc != PIKV_OK) return rc;
     if (!scores || !slot_coef || !n_valid || !topk_idx || !last_access || !freq)
         return PIKV_ERR_INVALID;
