@@ -500,8 +500,9 @@ def pikv_route_round_robin(rows, E, k, step, topk_idx, gates, stream=None):
     _check(st, "pikv_route_round_robin")
 
 
-# ---- Operators around an 8-bit cache.  What these pass on is checked here as well: the type of every tensor, and that all are
-# on one device, whose current stream they then use and which is current during the call.
+# ---- Operators around an 8-bit cache.  What these pass on is checked here as well: the type of every tensor, that all are
+# on one device, whose current stream they then use and which is current during the call, and that each holds what the
+# call reads or writes of it.
 def _typed(where, want, *tensors):
     for t in tensors:
         if t is not None and t.dtype != want:
@@ -513,11 +514,12 @@ def _storage(desc):
     return torch.float32 if desc.dtype == F32 else torch.bfloat16
 
 
-def _on_device(where, call, stream, *tensors):
-    """call(stream handle) with the tensors' device current."""
+def _on_device(where, call, stream, tensors):
+    """call(stream handle) with the tensors' device current.  ``tensors``: (name, tensor, the elements it must hold at least[, the
+    last dimension it must have if it has four])."""
     import torch
     device = None
-    for t in tensors:
+    for _, t, *_ in tensors:
         if t is None:
             continue
         if not t.is_cuda:
@@ -527,8 +529,19 @@ def _on_device(where, call, stream, *tensors):
         device = t.device
     if device is None:
         raise ValueError("%s: no tensor given" % where)
+    _holds(where, tensors)
     with torch.cuda.device(device):
         return call(_stream(stream))
+
+
+def _holds(where, tensors):
+    for name, t, least, *last in tensors:
+        if t is None:
+            continue
+        if t.numel() < least:
+            raise ValueError("%s: %s has %d elements, %d are needed" % (where, name, t.numel(), least))
+        if last and t.dim() == 4 and t.numel() > 0 and t.shape[-1] != last[0]:
+            raise ValueError("%s: the last dimension of %s is %d, not %d" % (where, name, t.shape[-1], last[0]))
 
 
 def _int32_float32(where, integers, floats, tables=()):
@@ -547,6 +560,43 @@ def _rows(x, token_stride):
     return x.data_ptr()
 
 
+def _rope_tensors(x, tokens, token_stride, Hq, Hkv, D, w_q, w_k, positions, inv_freq, rotary_dim, q_out, k_out, v_out):
+    row = (Hq + Hkv * (1 if v_out is None else 2)) * D
+    if x.is_contiguous():
+        rows = ("x", x, (tokens - 1) * token_stride + row if tokens > 0 else 0)
+    else:                                        # rows token_stride apart, each with what the view has of it
+        rows = ("x", x, max(tokens * x[:1].numel(), x.shape[0] * row if tokens > 0 else 0))
+    rotated = rotary_dim > 0
+    return [rows, ("w_q", w_q, D), ("w_k", w_k, D), ("positions", positions, tokens if rotated else 0),
+            ("inv_freq", inv_freq, rotary_dim // 2), ("q_out", q_out, tokens * Hq * D), ("k_out", k_out, tokens * Hkv * D),
+            ("v_out", v_out, tokens * Hkv * D)]
+
+
+def _cache_tensors(desc, block, K_shards, V_shards, K_scales, V_scales, n_valid):
+    be = desc.B * desc.E
+    blocks = (desc.S - 1) // block + 1 if block > 0 else 0
+    return [("K_shards", K_shards, be), ("V_shards", V_shards, be), ("K_scales", K_scales, be * desc.Hkv * blocks, blocks),
+            ("V_scales", V_scales, be * desc.Hkv * blocks, blocks), ("n_valid", n_valid, be)]
+
+
+def _append_tensors(desc, block, K_new, V_new, topk_idx, k, reuse_idx, reuse_cnt, max_evict, K_shards, V_shards, K_scales, V_scales,
+                    utility, n_valid):
+    be, row = desc.B * desc.E, desc.B * desc.Hkv * desc.D
+    return _cache_tensors(desc, block, K_shards, V_shards, K_scales, V_scales, n_valid) + [
+        ("K_new", K_new, row), ("V_new", V_new, row), ("topk_idx", topk_idx, desc.B * k), ("reuse_idx", reuse_idx, be * max_evict),
+        ("reuse_cnt", reuse_cnt, be), ("utility", utility, be * desc.S)]
+
+
+def _attn_tensors(desc, block, q, K_shards, V_shards, K_scales, V_scales, n_valid, topk_idx, gates, k, y, row_max, row_norm, scores,
+                  slot_coef, workspace):
+    heads = desc.B * desc.Hq
+    selected = desc.B * desc.route_rows_per_seq * k
+    return _cache_tensors(desc, block, K_shards, V_shards, K_scales, V_scales, n_valid) + [
+        ("q", q, heads * desc.D), ("topk_idx", topk_idx, selected), ("gates", gates, selected), ("y", y, heads * desc.D),
+        ("row_max", row_max, heads), ("row_norm", row_norm, heads), ("scores", scores, heads * k * desc.S, desc.S),
+        ("slot_coef", slot_coef, heads * k * 2), ("workspace", workspace, 0)]
+
+
 def pikv_norm_rope(x, tokens, token_stride, Hq, Hkv, D, w_q, w_k, eps, positions, inv_freq, rotary_dim, interleaved, q_out,
                    k_out, v_out=None, stream=None):
     """``x``: [tokens, heads * D] or [tokens, heads, D], rows ``token_stride`` elements apart (a view into a wider projection is
@@ -560,7 +610,7 @@ def pikv_norm_rope(x, tokens, token_stride, Hq, Hkv, D, w_q, w_k, eps, positions
         st = _on_device(where, lambda s: load_library().pikv_norm_rope(
             _rows(x, token_stride), tokens, token_stride, Hq, Hkv, D, _dtype_code(x), _p(w_q), _p(w_k), float(eps), _p(positions),
             _p(inv_freq), rotary_dim, 1 if interleaved else 0, _p(q_out), _p(k_out), _p(v_out), s),
-            stream, x, w_q, w_k, positions, inv_freq, q_out, k_out, v_out)
+            stream, _rope_tensors(x, tokens, token_stride, Hq, Hkv, D, w_q, w_k, positions, inv_freq, rotary_dim, q_out, k_out, v_out))
     if st != 0:
         _check(st, where)
 
@@ -575,7 +625,9 @@ def pikv_quant_pack(desc, format, block, K_dense, V_dense, dense_stride_h, dense
         _int32_float32(where, [n_valid], [K_scales, V_scales], [K_dense, V_dense, K_shards, V_shards])
         st = _on_device(where, lambda s: load_library().pikv_quant_pack(
             C.byref(desc), format, block, _p(K_dense), _p(V_dense), dense_stride_h, dense_stride_s, _p(n_valid), _p(K_shards),
-            _p(V_shards), _p(K_scales), _p(V_scales), s), stream, K_dense, V_dense, n_valid, K_shards, V_shards, K_scales, V_scales)
+            _p(V_shards), _p(K_scales), _p(V_scales), s), stream,
+            _cache_tensors(desc, block, K_shards, V_shards, K_scales, V_scales, n_valid) + [
+                ("K_dense", K_dense, desc.B * desc.E), ("V_dense", V_dense, desc.B * desc.E)])
     if st != 0:
         _check(st, where)
 
@@ -590,7 +642,9 @@ def pikv_quant_read(desc, format, block, K_shards, V_shards, K_scales, V_scales,
         _int32_float32(where, [n_valid], [K_scales, V_scales], [K_dense, V_dense, K_shards, V_shards])
         st = _on_device(where, lambda s: load_library().pikv_quant_read(
             C.byref(desc), format, block, _p(K_shards), _p(V_shards), _p(K_scales), _p(V_scales), _p(n_valid), _p(K_dense),
-            _p(V_dense), dense_stride_h, dense_stride_s, s), stream, K_shards, V_shards, K_scales, V_scales, n_valid, K_dense, V_dense)
+            _p(V_dense), dense_stride_h, dense_stride_s, s), stream,
+            _cache_tensors(desc, block, K_shards, V_shards, K_scales, V_scales, n_valid) + [
+                ("K_dense", K_dense, desc.B * desc.E), ("V_dense", V_dense, desc.B * desc.E)])
     if st != 0:
         _check(st, where)
 
@@ -605,8 +659,9 @@ def pikv_quant_append(desc, format, block, K_new, V_new, topk_idx, k, reuse_idx,
         _int32_float32(where, [topk_idx, reuse_idx, reuse_cnt, n_valid], [K_scales, V_scales, utility], [K_shards, V_shards])
         st = _on_device(where, lambda s: load_library().pikv_quant_append(
             C.byref(desc), format, block, _p(K_new), _p(V_new), _p(topk_idx), k, _p(reuse_idx), _p(reuse_cnt), max_evict,
-            _p(K_shards), _p(V_shards), _p(K_scales), _p(V_scales), _p(utility), _p(n_valid), s),
-            stream, K_new, V_new, topk_idx, reuse_idx, reuse_cnt, K_shards, V_shards, K_scales, V_scales, utility, n_valid)
+            _p(K_shards), _p(V_shards), _p(K_scales), _p(V_scales), _p(utility), _p(n_valid), s), stream,
+            _append_tensors(desc, block, K_new, V_new, topk_idx, k, reuse_idx, reuse_cnt, max_evict, K_shards, V_shards, K_scales,
+                            V_scales, utility, n_valid))
     if st != 0:
         _check(st, where)
 
@@ -628,7 +683,7 @@ def pikv_quant_attn(desc, format, block, q, K_shards, V_shards, K_scales, V_scal
         st = _on_device(where, lambda s: load_library().pikv_quant_attn(
             C.byref(desc), format, block, _p(q), _p(K_shards), _p(V_shards), _p(K_scales), _p(V_scales), _p(n_valid), _p(topk_idx),
             _p(gates), k, combine, float(scale), _p(y), _p(row_max), _p(row_norm), _p(scores), _p(slot_coef), _p(workspace), ws_bytes,
-            s), stream, q, K_shards, V_shards, K_scales, V_scales, n_valid, topk_idx, gates, y, row_max, row_norm, scores, slot_coef,
-            workspace)
+            s), stream, _attn_tensors(desc, block, q, K_shards, V_shards, K_scales, V_scales, n_valid, topk_idx, gates, k, y, row_max,
+                                      row_norm, scores, slot_coef, workspace))
     if st != 0:
         _check(st, where)

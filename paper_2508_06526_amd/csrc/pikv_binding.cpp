@@ -65,6 +65,9 @@ struct Args {
     bool usual = true;                   // every argument so far was of the ordinary kind (no exception: one costs as much as a call)
     at::ScalarType dense = at::ScalarType::Undefined;      // strict: the type of Dense tensors, the descriptor's or the first one's
     bool strict = false;                 // the tensors of int32_t *, float * and tables are of that type (tables: int64), and all are on one device
+    // strict: what the tensor at each place holds, and its last dimension if it has four; a tensor that is not given holds anything
+    static constexpr int kPlaces = 20;
+    int64_t held[kPlaces], last_of_four[kPlaces];
 
     template <typename T>
     T unusual() {
@@ -72,10 +75,16 @@ struct Args {
         return T{};
     }
     const at::Tensor *tensor(PyObject *o) {
+        const int64_t place = at - 1 - begin;
+        if (strict && place < kPlaces) held[place] = INT64_MAX, last_of_four[place] = -1;
         if (o == Py_None) return nullptr;
         if (!THPVariable_CheckExact(o)) return unusual<const at::Tensor *>();
         const at::Tensor &t = THPVariable_Unpack(o);
         if (strict && first != nullptr && t.device() != first->device()) return unusual<const at::Tensor *>();
+        if (strict && place < kPlaces) {
+            held[place] = t.numel();
+            if (t.dim() == 4 && t.numel() > 0) last_of_four[place] = t.size(3);
+        }
         return t.is_cuda() && t.is_contiguous() ? &t : unusual<const at::Tensor *>();
     }
     template <typename T>
@@ -206,6 +215,41 @@ struct OnDevice {
     }
 };
 
+// Whether the tensors of a strict call hold what the call reads and writes of them (binding.py: *_tensors; it reports what is short).
+template <Function F, typename VALUES>
+bool all_hold(const Args &a, const VALUES &v) {
+    typedef __int128 Count;                  // a product of four sizes
+    auto holds = [&](int place, Count least) { return (Count)a.held[place] >= least; };
+    if constexpr (F == kNormRope) {
+        const Count tokens = std::get<1>(v), stride = std::get<2>(v), Hq = std::get<3>(v), Hkv = std::get<4>(v), D = std::get<5>(v);
+        const int rotary = std::get<12>(v);
+        const Count row = (Hq + Hkv * (std::get<16>(v) != nullptr ? 2 : 1)) * D;
+        return holds(0, tokens > 0 ? (tokens - 1) * stride + row : 0) && holds(6, D) && holds(7, D) && holds(9, rotary > 0 ? tokens : 0) &&
+               holds(10, rotary / 2) && holds(13, tokens * Hq * D) && holds(14, tokens * Hkv * D) && holds(15, tokens * Hkv * D);
+    } else if constexpr (F == kQuantPack || F == kQuantRead || F == kQuantAppend || F == kQuantAttn) {
+        const pikv_desc &d = *std::get<0>(v);
+        const int block = std::get<2>(v), blocks = block > 0 ? (d.S - 1) / block + 1 : 0;
+        const Count be = (Count)d.B * d.E;
+        auto scales = [&](int place) { return holds(place, be * d.Hkv * blocks) && (a.last_of_four[place] < 0 || a.last_of_four[place] == blocks); };
+        if constexpr (F == kQuantPack)
+            return holds(3, be) && holds(4, be) && holds(7, be) && holds(8, be) && holds(9, be) && scales(10) && scales(11);
+        if constexpr (F == kQuantRead)
+            return holds(3, be) && holds(4, be) && scales(5) && scales(6) && holds(7, be) && holds(8, be) && holds(9, be);
+        if constexpr (F == kQuantAppend) {
+            const Count rows = (Count)d.B * d.Hkv * d.D, k = std::get<6>(v), max_evict = std::get<9>(v);
+            return holds(3, rows) && holds(4, rows) && holds(5, d.B * k) && holds(7, be * max_evict) && holds(8, be) && holds(10, be) &&
+                   holds(11, be) && scales(12) && scales(13) && holds(14, be * d.S) && holds(15, be);
+        }
+        if constexpr (F == kQuantAttn) {
+            const Count heads = (Count)d.B * d.Hq, k = std::get<11>(v), selected = (Count)d.B * d.route_rows_per_seq * k;
+            return holds(3, heads * d.D) && holds(4, be) && holds(5, be) && scales(6) && scales(7) && holds(8, be) && holds(9, selected) &&
+                   holds(10, selected) && holds(14, heads * d.D) && holds(15, heads) && holds(16, heads) && holds(17, heads * k * d.S) &&
+                   (a.last_of_four[17] < 0 || a.last_of_four[17] == d.S) && holds(18, heads * k * 2);
+        }
+    }
+    return true;
+}
+
 template <Function F, typename FN, typename... KINDS>
 struct Caller;
 template <Function F, typename... A, typename... KINDS>
@@ -220,7 +264,7 @@ struct Caller<F, int (*)(A...), KINDS...> {
             a.strict = strict;
             // (braces: the arguments are taken from left to right)
             const std::tuple<A...> values{Take<A, typename KindOf<(int)I, KINDS...>::type>::from(a)...};
-            if (!a.usual || a.first == nullptr) Py_RETURN_NONE;
+            if (!a.usual || a.first == nullptr || !all_hold<F>(a, values)) Py_RETURN_NONE;
             auto call = [&]() noexcept { return std::apply(reinterpret_cast<int (*)(A...)>(addresses[F]), values); };
             auto call_there = [&] {
                 if constexpr (strict) {
