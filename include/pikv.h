@@ -468,7 +468,8 @@ size_t pikv_quant_attn_workspace_bytes(const pikv_desc *desc, int32_t k);
  * feed pikv_update_utility.  A selected index outside 0..E-1 counts as an empty shard here.  The workspace holds
  * nothing between calls; calls that may overlap (streams, captured graphs) need one each.
  * Errors: as pikv_sharded_attn; UNSUPPORTED as above, for tq > 1 with per-head routing, stride_s above 2^24
- * bytes and 2^23 blocks of work or more.                                                                 */
+ * bytes, 2^23 blocks of work or more, and B * Hq >= 2^22 query rows (2^24 while k times the splits of a shard is at
+ * most 32) where a launch of its own merges the blocks' results.                                         */
 int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t block, const void *q,
                     const void *const *K_shards, const void *const *V_shards, const float *K_scales,
                     const float *V_scales, const int32_t *n_valid, const int32_t *topk_idx, const float *gates,

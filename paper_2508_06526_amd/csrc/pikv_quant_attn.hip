@@ -485,6 +485,8 @@ int make_plan(const pikv_desc *d, int k, QuantPlan *plan) {
     plan->chunk = (int)chunk;
     plan->nsplit = (int)((d->S + chunk - 1) / chunk);
     if (units * plan->nsplit >= (1 << 23)) return PIKV_ERR_UNSUPPORTED;
+    // A launch has fewer than 2^32 threads; the merge's have a block for every query row.
+    if (!plan->merged && (int64_t)d->B * d->Hq * combine_threads(k * plan->nsplit) >= (int64_t)1 << 32) return PIKV_ERR_UNSUPPORTED;
     const size_t partials = (size_t)d->B * d->Hq * k * plan->nsplit;
     plan->acc_bytes = (partials * d->D * sizeof(float) + 255) / 256 * 256;
     plan->ml_bytes = (partials * 2 * sizeof(float) + 255) / 256 * 256;
