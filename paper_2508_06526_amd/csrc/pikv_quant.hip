@@ -342,7 +342,6 @@ int quant_tiles(const pikv_desc *desc, int format, int block, int slots, const v
                 float *V_scales, QuantParams *p, unsigned *grid) {
     const int rc = check_quant(desc, format, block);
     if (rc != PIKV_OK) return rc;
-    if (!K_dense || !V_dense || !n_valid || !K || !V || !K_scales || !V_scales) return PIKV_ERR_INVALID;
     const int eb = elem_bytes(desc->dtype);
     if (dense_s < desc->D || (dense_s * eb) % 16 != 0 || dense_h < 0 || (dense_h * eb) % 16 != 0) return PIKV_ERR_INVALID;
     if (desc->Hkv > 1 && dense_h < (int64_t)(desc->S - 1) * dense_s + desc->D) return PIKV_ERR_INVALID;
@@ -350,6 +349,9 @@ int quant_tiles(const pikv_desc *desc, int format, int block, int slots, const v
     // (a launch has fewer than 2^32 threads)
     const int64_t per_sequence = (int64_t)desc->E * desc->Hkv * 2 * tiles, most = ((int64_t)1 << 23) - 1;
     if (desc->B > 0 && per_sequence > most / desc->B) return PIKV_ERR_UNSUPPORTED;
+    *grid = (unsigned)(desc->B * per_sequence);
+    if (*grid == 0) return PIKV_OK;              // (tensors without elements have no address)
+    if (!K_dense || !V_dense || !n_valid || !K || !V || !K_scales || !V_scales) return PIKV_ERR_INVALID;
     p->K_dense = K_dense;
     p->V_dense = V_dense;
     p->K = K;
@@ -367,7 +369,6 @@ int quant_tiles(const pikv_desc *desc, int format, int block, int slots, const v
     p->S = desc->S;
     p->n_blocks = (desc->S - 1) / block + 1;
     p->block_bits = __builtin_ctz(block);
-    *grid = (unsigned)(desc->B * per_sequence);
     return PIKV_OK;
 }
 
@@ -418,10 +419,12 @@ extern "C" int pikv_quant_append(const pikv_desc *desc, int32_t format, int32_t 
                                  float *V_scales, float *utility, int32_t *n_valid, void *stream) {
     const int rc = check_quant(desc, format, block);
     if (rc != PIKV_OK) return rc;
-    if (!K_new || !V_new || !topk_idx || !K_shards || !V_shards || !K_scales || !V_scales || !utility || !n_valid)
-        return PIKV_ERR_INVALID;
     if (k < 1 || k > desc->E) return PIKV_ERR_INVALID;
-    if ((reuse_idx == nullptr) != (reuse_cnt == nullptr)) return PIKV_ERR_INVALID;
+    if (desc->B != 0) {                          // (tensors without elements have no address)
+        if (!K_new || !V_new || !topk_idx || !K_shards || !V_shards || !K_scales || !V_scales || !utility || !n_valid)
+            return PIKV_ERR_INVALID;
+        if ((reuse_idx == nullptr) != (reuse_cnt == nullptr)) return PIKV_ERR_INVALID;
+    }
     if (reuse_idx && max_evict < 1) return PIKV_ERR_INVALID;
     if (desc->route_rows_per_seq != 1) return PIKV_ERR_UNSUPPORTED;   // one insert per sequence
     if ((int64_t)desc->B * k > (1 << 21)) return PIKV_ERR_UNSUPPORTED;

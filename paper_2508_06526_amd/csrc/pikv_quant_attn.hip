@@ -515,10 +515,10 @@ extern "C" int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t bl
     QuantPlan plan;
     rc = make_plan(desc, k, &plan);
     if (rc != PIKV_OK) return rc;
-    if (!q || !K_shards || !V_shards || !K_scales || !V_scales || !n_valid || !topk_idx || !y) return PIKV_ERR_INVALID;
     if (combine != PIKV_COMBINE_LSE && combine != PIKV_COMBINE_LOCAL) return PIKV_ERR_INVALID;
     if (!(scale == scale)) return PIKV_ERR_INVALID;
-    if (desc->B == 0) return PIKV_OK;
+    if (desc->B == 0) return PIKV_OK;            // (tensors without elements have no address)
+    if (!q || !K_shards || !V_shards || !K_scales || !V_scales || !n_valid || !topk_idx || !y) return PIKV_ERR_INVALID;
     if (!workspace || workspace_bytes_given < workspace_bytes(plan)) return PIKV_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return PIKV_ERR_INVALID;
     const int tq = desc->tq > 1 ? desc->tq : 1;

@@ -114,13 +114,13 @@ extern "C" int pikv_norm_rope(const void *x, int32_t tokens, int64_t token_strid
     if (D != 16 && D != 32 && D != 64 && D != 128) return PIKV_ERR_UNSUPPORTED;
     if (rotary_dim < 0 || rotary_dim > D || rotary_dim % 16 != 0) return PIKV_ERR_INVALID;
     if (!(eps >= 0.0f) || eps > 3.0e38f) return PIKV_ERR_INVALID;
-    if (!x || (Hq > 0 && !q_out) || (Hkv > 0 && !k_out) || (rotary_dim > 0 && (!positions || !inv_freq))) return PIKV_ERR_INVALID;
     const int64_t heads = (int64_t)Hq + (int64_t)Hkv * (v_out ? 2 : 1);
     if (heads > (1 << 20)) return PIKV_ERR_UNSUPPORTED;
     if (token_stride < heads * D || (token_stride * elem_bytes(dtype)) % 16 != 0) return PIKV_ERR_INVALID;
+    if (tokens == 0) return PIKV_OK;             // (tensors without elements have no address)
+    if (!x || (Hq > 0 && !q_out) || (Hkv > 0 && !k_out) || (rotary_dim > 0 && (!positions || !inv_freq))) return PIKV_ERR_INVALID;
     auto aligned = [](const void *ptr) { return reinterpret_cast<uintptr_t>(ptr) % 16 == 0; };
     if (!aligned(x) || !aligned(w_q) || !aligned(w_k) || !aligned(q_out) || !aligned(k_out) || !aligned(v_out)) return PIKV_ERR_INVALID;
-    if (tokens == 0) return PIKV_OK;
     RopeParams p;
     p.x = x;
     p.w_q = w_q;
