@@ -380,7 +380,7 @@ int pikv_policy_compact(const pikv_desc *desc, const int32_t *evicted_idx, const
  * rotation, in one pass (Algorithm 1 takes K_t, V_t and q_t as given; "K is stored post-rotation" in
  * every call above).  Per token t and head, x its D values:
  *     z = x * w / sqrt(mean(x^2) + eps)             (w = w_q or w_k, shared by the heads; NULL: z = x)
- *     angle_i = positions[t] * inv_freq[i], i < rotary_dim / 2, not rounded below 64 bits
+ *     angle_i = positions[t] * inv_freq[i], i < rotary_dim / 2, in 64 bits up to its cosine and sine
  *     (z_a, z_b) -> (z_a cos - z_b sin, z_b cos + z_a sin) on the pairs (i, i + rotary_dim / 2), or
  *     (2 i, 2 i + 1) with `interleaved`; values from rotary_dim on stay z
  * in fp32, rounded once to the storage type.

@@ -11,7 +11,8 @@
 // that are in them 8.1 instead of 6.9).
 //
 // Angle = position * inv_freq: in fp32 the product of a far position is off by its own rounding (position 10^6: 0.03
-// radians), so it is formed in 64 bits, in revolutions, and only what is left after whole ones is rounded.
+// radians), so it is formed in 64 bits, in revolutions; what is left after whole ones goes into cosine and sine as an fp32
+// value and its remainder.
 #include "pikv_mfma_dev.h"
 
 #include <math.h>
@@ -46,7 +47,12 @@ __global__ __launch_bounds__(kRopeThreads) void norm_rope(RopeParams p) {
     uint4 next = load(first);                // ahead of the angles
     if (tid < half) {
         const double turns = (double)p.positions[token] * (double)p.inv_freq[tid] * 0.15915494309189533577;      // 1 / (2 pi)
-        sincospif((float)(2.0 * (turns - rint(turns))), &sin_s[tid], &cos_s[tid]);
+        const double half_turns = 2.0 * (turns - rint(turns));
+        const float near = (float)half_turns, rest = (float)((half_turns - near) * M_PI);
+        float sn, cs;
+        sincospif(near, &sn, &cs);
+        sin_s[tid] = fmaf(rest, cs, sn);         // what the rounding of the angle left, to first order (its square: 2^-47)
+        cos_s[tid] = fmaf(-rest, sn, cs);
     }
     __syncthreads();
     for (int head = first; head < last; head += STEP) {
@@ -71,9 +77,13 @@ __global__ __launch_bounds__(kRopeThreads) void norm_rope(RopeParams p) {
             for (int i = 0; i < VPL; ++i) sum = fmaf(z[i], z[i], sum);
 #pragma unroll
             for (int off = 1; off < LPR; off <<= 1) sum += __shfl_xor(sum, off, kWave);
-            const float r = 1.0f / sqrtf(sum * (1.0f / D) + p.eps);
+            // r + rest = 1 / sqrt(v): r is off by the roundings of root and division, and rest is what they took (a step of Newton's,
+            // r (1 - v r^2) / 2), so that the product is the only rounding of x / sqrt(v)
+            const float v = sum * (1.0f / D) + p.eps, r = 1.0f / sqrtf(v);
+            const float vr = v * r, vr_low = fmaf(v, r, -vr), left = fmaf(-vr, r, 1.0f) - vr_low * r;
+            const float rest = r > 0.0f && r < INFINITY ? 0.5f * left * r : 0.0f;
 #pragma unroll
-            for (int i = 0; i < VPL; ++i) z[i] = z[i] * r * load_scalar<T>(w, VPL * c + i);
+            for (int i = 0; i < VPL; ++i) z[i] = fmaf(z[i], r, z[i] * rest) * load_scalar<T>(w, VPL * c + i);
         }
         if (VPL * c < p.rotary) {                       // (rotary: a multiple of 16; a head's rotated lanes are whole pairs)
             if (p.interleaved) {
