@@ -553,7 +553,7 @@ def _int32_float32(where, integers, floats, tables=()):
 
 def _rows(x, token_stride):
     """Device address of rows that need not be contiguous: a slice of a wider projection."""
-    if (x.stride(-1) != 1 and x.shape[-1] > 1) or (x.dim() > 2 and x.stride(1) != x.shape[2]):
+    if (x.stride(-1) != 1 and x.shape[-1] > 1) or (x.dim() > 2 and x.shape[1] > 1 and x.stride(1) != x.shape[2]):
         raise ValueError("the values of a row must be contiguous")
     if x.dim() > 1 and not x.is_contiguous() and x.stride(0) != token_stride:
         raise ValueError("rows are %d elements apart, token_stride is %d" % (x.stride(0), token_stride))

@@ -79,3 +79,11 @@ def test_rows_of_a_projection():
                   (z(5, 16 * D), dict(token_stride=20 * D))):
         with pytest.raises(ValueError, match="call: x"):
             binding._holds("call", rope(x=x, **kw))
+
+
+def test_rows_of_one_head_may_be_a_slice_of_a_wider_one():
+    wide = z(5, 1, 100)
+    assert binding._rows(wide[:, :, 20:84], 100) == wide.data_ptr() + 80
+    for x in (z(5, 2, 100)[:, :, 20:84], z(5, 64, 2).transpose(1, 2)[:, :1]):          # heads that do not follow each other, values that do not
+        with pytest.raises(ValueError, match="contiguous"):
+            binding._rows(x, 200)
