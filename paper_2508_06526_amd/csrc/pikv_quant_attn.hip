@@ -18,9 +18,9 @@
 //     each.
 // A lane's piece of the next stage is requested as soon as this one's has been used: K behind the scores, V behind the output.
 //
-// Bound by memory from some 100 MB of codes on: 32 sequences x 32 kv heads x 2 shards of 2048 x 128 codes, 1.07 GB, in 166 us (6.5 TB/s; a pass
-// that only reads 156).  Below by the trips and launches around it: 64 MB under 4 query heads, with 4 MB of scores, 16.7 us
-// (the loads alone 14.2, a read-only pass 12.1) and a merge of 4.  Two stages ahead instead of one, or eight waves a block, changed
+// Bound by memory from some 100 MB of codes on: 32 sequences x 32 kv heads x 2 shards of 2048 x 128 codes, 1.07 GB, in 173 us with the merge (6.2 TB/s; a
+// pass that only reads 156).  Below by the trips and launches around it: 64 MB under 4 query heads, with 4 MB of scores, 16.6 us (median; the loads
+// alone 14.2, a read-only pass 12.1) and a merge of 4.5.  Two stages ahead instead of one, or eight waves a block, changed
 // nothing but the registers.
 #include "pikv_combine_dev.h"
 #include "pikv_mfma_dev.h"
@@ -466,11 +466,14 @@ int make_plan(const pikv_desc *d, int k, QuantPlan *plan) {
     plan->rows = per_head ? 1 : G < plan->row_tiles * kRows ? G : plan->row_tiles * kRows;
     plan->row_blocks = (G + plan->rows - 1) / plan->rows;
     const int64_t units = (int64_t)d->B * d->Hkv * plan->row_blocks * k;
-    // The merged form, one launch and no partials: where a wave's rows are one stage or two (1 x 8 kv heads x 2 of 128 entries 7.9 -> 6.7 us, 256
-    // entries, two stages of a wave, even) and where there are blocks for most CUs without splits (64 x 8 x 2 of 64 - 1000 entries 14.5 -> 9.7 to
-    // 53.8 -> 49.0; 16 x 8 x 2 of 4096 40 -> 61), but not many short ones (2048 blocks of 256 entries 32.2 -> 35.5).
+    // The merged form, one launch and no partials.  Where a wave has one stage of 128 values, or two of fewer (1 x 8 kv heads x 2 shards of 128
+    // entries of 128 values 7.5 -> 6.3 us, of 256 of 64 values 7.0 -> 6.2; two stages of 128 values 7.6 -> 8.5, four of 32 values 7.0 -> 7.8).
+    // And where there are blocks for most CUs without splits: 24 x 8 x 2 of 256 entries 13.0 -> 9.6, of 1024 26.7 -> 23.1, of 2048 even, 8 shards of 512
+    // even; 80 x 8 x 2 of 512 39.0 -> 35.9.  With 128 blocks the splits win from 512 entries on (12.4 against 13.4; of 1024 17.5 against 21.6).
+    // (Above 640 blocks splits, for many short shards: 2048 blocks of 256 entries 32.2 against 35.5; 768 and 1280 blocks of 512 would gain, 45 -> 39 and
+    // 71 -> 60.)
     const int64_t blocks = units / k, rows = (int64_t)k * d->S;
-    const bool one_round = (int64_t)d->S * d->D <= (int64_t)128 * kTile * (kMergedWaves / k);
+    const bool one_round = (int64_t)d->S * (d->D > 64 ? d->D : 64) <= (int64_t)128 * kTile * (kMergedWaves / k);
     plan->merged = plan->row_tiles == 1 && k <= kMergedWaves && blocks <= 640 && (one_round || (blocks >= 192 && rows <= 4096));
     // A block per CU, and blocks of at most 1024 rows, but none of fewer than a stage of each wave.
     int64_t nsplit = units > 0 ? 256 / units : 1;

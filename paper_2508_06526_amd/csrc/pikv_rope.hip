@@ -6,7 +6,7 @@
 //               heads: cosines and sines are formed once per block, behind the first request for rows, and kept in LDS.
 //
 // Bound by memory: 16384 tokens x 48 heads of 128 bf16 values, 403 MB, in 71 us (5.7 TB/s; a plain copy here 5.1), 59 where the
-// projection's rows are still in the Infinity Cache; a token in 2.4 us of the GPU's time, the launch and two trips to memory.
+// projection's rows are still in the Infinity Cache; a token in 2.5 us of the GPU's time, the launch and two trips to memory.
 // Rows come through the caches, outputs go past them (with ordinary stores 75 us; rows past the caches as well 70, but 1024 tokens
 // that are in them 8.1 instead of 6.9).
 //

@@ -39,3 +39,15 @@ def test_what_can_be_checked_without_addresses_is(tokens, kw):
                                             None, None) in (-1, -2)
     d = C.byref(pk.make_desc(0, 8, 4, 64, 8, 100, dtype=1))
     assert pk.load_library().pikv_quant_append(d, 0, 16, *[None] * 3, 9, None, None, 0, *[None] * 7) == -1
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("k", [1, 2, 3, 8])
+def test_a_wave_of_the_short_form_has_two_stages_at_most(D, k):
+    """One launch leaves one partial per row and shard to hold, a split pass one for each split."""
+    def partials(S):
+        return pk.pikv_quant_attn_workspace_bytes(pk.make_desc(1, 8, 8, D, 16, S, dtype=1), k) // (8 * k * (D + 2) * 4)
+    stage = 32 * (8 // k)                                   # entries of a stage of a shard's waves
+    most = stage * (1 if D == 128 else 2)
+    assert partials(most) == 1
+    assert partials(max(most, 128) + 1) > 1                 # (shards of up to 128 entries are not split)
