@@ -408,7 +408,7 @@ int pikv_norm_rope(const void *x, int32_t tokens, int64_t token_stride, int32_t 
  *   format  pikv_quant_format; block: 16, 32, 64 or 128 slots that share a scale
  *   K_scales, V_scales [B,E,Hkv,ceil(S/block)] float32: one scale per block of slots
  *           and kv head, K and V apart.  Entry i of a row stands for code_i * scale.
- * Scales are powers of two (or 0 where nothing has been written: zeros): as pikv_quant_pack writes them, the smallest one,
+ * Scales are powers of two (or 0 where nothing has been written: zeros, if the bytes there are no NaN of e4m3): as pikv_quant_pack writes them, the smallest one,
  * 2^-126 at the least, that brings the largest magnitude of the block's rows within the largest code (127 or 448).
  * Divisions by it are then exact, a code as it is written is the nearest one (ties to even) to x / scale, and the value it
  * stands for is exact in either dense type unless it underflows - every call here gives the same bits on
