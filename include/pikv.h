@@ -476,6 +476,110 @@ int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t block, const 
                     int32_t k, int32_t combine, float scale, float *y, float *row_max, float *row_norm,
                     float *scores, float *slot_coef, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- From a prompt to a paged cache ----
+ * Scores of the calls below, of query i at position p_i and entry j at p_j, head h:
+ *     s = scale <q_i, k_j>;   cap > 0: s = cap tanh(s / cap);   slopes: s = s - slopes[h] |p_i - p_j|
+ * and j is seen by i where  p_j < prefix  or  (p_j <= p_i and (window <= 0 or p_i - p_j < window)); a prefix is seen by all
+ * tokens of its sequence, window or not (its own among them: both ways), what is not seen has weight zero, whatever it
+ * holds.  scale <= 0 selects 1/sqrt(D).
+ *
+ * Prompts are packed: the tokens of sequence b are rows cu_seqlens[b] .. cu_seqlens[b+1]-1 of [tokens, ...] arrays, their positions
+ * count from 0, and no sequence sees another.  Rows in no sequence, and those of a sequence from max_len on, are neither read nor
+ * written.
+ *
+ * pikv_prompt_attn: attention of the prompts among themselves, what the layers of the model need on the way to a cache.
+ *   q [tokens, Hq, D], k, v [tokens, Hkv, D] dtype; tokens are q_stride / k_stride / v_stride elements apart (at least a
+ *             row, multiples of 16 bytes; heads are D apart), on 16-byte boundaries
+ *   cu_seqlens [B+1] int32, ascending, within 0..tokens;  max_len: the longest sequence, or more
+ *   prefix    [B] int32 or NULL;  slopes [Hq] float32 or NULL
+ *   out       [tokens, Hq, D] dtype out: rows go on into a projection of the storage type
+ *   row_max, row_norm [tokens, Hq] float32 out or both NULL: the largest score of the row and sum_j exp(s_j - row_max)
+ * Errors: INVALID for null required pointers, one of row_max and row_norm without the other, tokens, B or max_len < 0, Hq or Hkv < 1, Hq % Hkv != 0, strides or
+ * addresses as above, cap < 0, cap or scale NaN or infinite, unknown dtype; UNSUPPORTED for D other than 32, 64, 128, Hq > 256, tokens > 2^23 or 2^23
+ * blocks of work and more (128 rows of a kv head's queries each).  tokens == 0, B == 0 and max_len == 0 are no-ops. */
+int pikv_prompt_attn(const void *q, const void *k, const void *v, int32_t tokens, int64_t q_stride, int64_t k_stride,
+                     int64_t v_stride, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype, const int32_t *cu_seqlens, int32_t B,
+                     int32_t max_len, const int32_t *prefix, float scale, float cap, const float *slopes, int32_t window, void *out,
+                     float *row_max, float *row_norm, void *stream);
+
+/* Bytes of scratch pikv_prompt_mass needs (host computation; 0 for sizes it refuses).  256-byte aligned.                */
+size_t pikv_prompt_mass_workspace_bytes(int32_t tokens, int32_t Hkv, int32_t B, int32_t max_len);
+
+/* Section 3.4, Table 3 row H2O over a prompt: the attention each of its entries got from all of its tokens and query heads,
+ *     mass[j] = sum_h sum_i exp(s_ij - row_max[i][h]) / row_norm[i][h]      over the tokens i that see j,
+ * the utility its entry starts with (pikv_paged_fill's weight).  Arguments as pikv_prompt_attn, which leaves row_max and row_norm;
+ * they are inputs here.  A row whose row_norm is 0 gives nothing.
+ *   mass      [tokens] float32 out
+ * Sums run in a fixed order.  The workspace holds nothing between calls; calls that may overlap need one each.
+ * Errors: as pikv_prompt_attn; WORKSPACE if workspace_bytes is too small.                                              */
+int pikv_prompt_mass(const void *q, const void *k, int32_t tokens, int64_t q_stride, int64_t k_stride, int32_t Hq, int32_t Hkv,
+                     int32_t D, int32_t dtype, const int32_t *cu_seqlens, int32_t B, int32_t max_len, const int32_t *prefix,
+                     float scale, float cap, const float *slopes, int32_t window, const float *row_max, const float *row_norm,
+                     float *mass, void *workspace, size_t workspace_bytes, void *stream);
+
+/* A paged cache: slot i of shard (b, e) lies in page page_table[b][e][i / page], at slot i % page of it; pages are parts of one
+ * pool of K rows and one of V rows, which shards of other requests may share.  Slots keep their numbers, so pikv_route, pikv_evict
+ * with compact == 0, the pikv_policy calls and the utility updates serve such a cache as they are.
+ *   pikv_pages  geometry of both pools, in elements: page p, kv head h', slot s of it start at
+ *               p * stride_page + h' * stride_h + s * stride_s, D values each, on 16-byte boundaries; no two rows may overlap
+ *   K_pool, V_pool  dtype;  page_table [B,E,ceil(S/page)] int32; an entry outside 0..n_pages-1 is no page
+ *   entry_pos   [B,E,S] int32: positions (>= 0) of the entries, or NULL where nothing goes by them
+ * In the descriptor D is 32, 64 or 128, rank 0 and flags 0 (UNSUPPORTED / INVALID otherwise); S is the capacity in slots;
+ * its strides mean nothing here.                                                                          */
+typedef struct pikv_pages {
+    int32_t n_pages;      /* of the pools                                                  */
+    int32_t page;         /* slots of a page: 16, 32, 64, 128 or 256                       */
+    int64_t stride_page, stride_h, stride_s;
+} pikv_pages;
+
+/* The rows of packed prompts into the shards their tokens selected (Algorithm 1, Insert, for all tokens of a prompt at once): in
+ * shard (b, e) the tokens of sequence b that list e take the slots from n_valid[b][e] on, in their order.  If there are more of them than
+ * the shard has room for - up to S, and to its first missing page - those of the largest weight stay (equal ones: the earlier token; a NaN
+ * ranks below all; without weights the earliest), in the tokens' order: Section 3.4's bounded memory, without a row written that goes at once.
+ *   K_new, V_new [tokens,Hkv,D] dtype;  cu_seqlens [B+1] as above
+ *   topk_idx  [tokens,k] int32: an index outside 0..E-1 is no shard, one listed twice takes the entry once
+ *   weight    [tokens] float32 or NULL;  positions [tokens] int32, given with entry_pos or not at all
+ *   utility   [B,E,S] float32: of a new entry its token's weight (0 without weights);  n_valid [B,E] int32, in place
+ *   slots     [tokens,k] int32 out: the slot of token t in its j-th shard, -1 where it has none (of an index listed twice the
+ *             first has it); rows of tokens in no sequence are left
+ * Errors: descriptor and page errors, INVALID for null required pointers, k not in 1..E, tokens < 0, K_new or V_new not on 16-byte boundaries;
+ * UNSUPPORTED for tokens > 2^23 and route_rows_per_seq != 1.  tokens == 0 and B == 0 are no-ops.                */
+int pikv_paged_fill(const pikv_desc *desc, const pikv_pages *pages, const void *K_new, const void *V_new, int32_t tokens,
+                    const int32_t *cu_seqlens, const int32_t *topk_idx, int32_t k, const float *weight, const int32_t *positions,
+                    void *K_pool, void *V_pool, const int32_t *page_table, int32_t *entry_pos, float *utility, int32_t *n_valid,
+                    int32_t *slots, void *stream);
+
+/* pikv_append for these shards: the same slot rule, utility and count; an entry whose slot has no page is dropped, as one of a full
+ * shard is.  positions [B] int32, given with entry_pos or not at all.  An index outside 0..E-1 is no shard, one listed twice
+ * takes the entry once.
+ * Errors: descriptor and page errors, INVALID for null required pointers, k not in 1..E, one of reuse_idx and reuse_cnt without the other,
+ * max_evict < 1 with them, K_new or V_new not on 16-byte boundaries; UNSUPPORTED for B * k > 2^21 and route_rows_per_seq != 1. */
+int pikv_paged_append(const pikv_desc *desc, const pikv_pages *pages, const void *K_new, const void *V_new, const int32_t *topk_idx,
+                      int32_t k, const int32_t *reuse_idx, const int32_t *reuse_cnt, int32_t max_evict, const int32_t *positions,
+                      void *K_pool, void *V_pool, const int32_t *page_table, int32_t *entry_pos, float *utility, int32_t *n_valid,
+                      void *stream);
+
+/* Bytes of scratch pikv_paged_attn needs (host computation; 0 if the descriptor is invalid or not supported).
+ * The workspace must be 256-byte aligned.                                                                 */
+size_t pikv_paged_attn_workspace_bytes(const pikv_desc *desc, int32_t k);
+
+/* pikv_sharded_attn over these shards, with the scores above: same meaning of every argument, both combine modes, per-token and
+ * per-head routing, desc->tq > 1 (the multi-query layout above) for either dtype, every D here and any group size.
+ *   slopes    [Hq / tq] float32 or NULL;  prefix [B] int32 or NULL;  q_pos [B,tq] int32: positions of the queries
+ * Where slopes, a window or a prefix is given, entry_pos and q_pos are too; where entry_pos is given, entries that a query does not
+ * see (later ones among them: drafts that have been appended see each other causally) have the score -inf, and
+ * an entry with a negative position is seen by none.  Without entry_pos every valid entry is seen.
+ * scores + slot_coef feed pikv_update_utility.  A selected index outside 0..E-1 counts as an empty shard, entries in a missing
+ * page as not seen.  The workspace holds nothing between calls; calls that may overlap (streams, captured graphs) need one each.
+ * Errors: as pikv_sharded_attn; descriptor and page errors; INVALID for one of entry_pos and q_pos without the other, or neither with slopes, a
+ * window or a prefix, cap < 0, cap or scale NaN or infinite; UNSUPPORTED for tq > 1 with per-head routing, stride_s above 2^24 bytes, and 2^23 blocks
+ * of work or more.                                                                                        */
+int pikv_paged_attn(const pikv_desc *desc, const pikv_pages *pages, const void *q, const void *K_pool, const void *V_pool,
+                    const int32_t *page_table, const int32_t *n_valid, const int32_t *topk_idx, const float *gates, int32_t k,
+                    int32_t combine, float scale, float cap, const float *slopes, int32_t window, const int32_t *prefix,
+                    const int32_t *entry_pos, const int32_t *q_pos, float *y, float *row_max, float *row_norm, float *scores,
+                    float *slot_coef, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Tuning hook: force the number of row-range splits per (head group, selected shard) used
  * by pikv_sharded_attn and pikv_attn_workspace_bytes (process-wide; 0 restores the built-in
  * choice of one round of resident blocks).  Change it only between calls, and size the

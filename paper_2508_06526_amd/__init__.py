@@ -6,7 +6,8 @@ There is no CPU or eager fallback: if the library is missing, calls raise.
 """
 from .binding import (  # noqa: F401
     BF16, F32, QUANT_E4M3, QUANT_INT8, pikv_norm_rope, pikv_quant_append, pikv_quant_attn, pikv_quant_attn_workspace_bytes,
-    pikv_quant_pack, pikv_quant_read,
+    pikv_quant_pack, pikv_quant_read, PikvPages, make_pages, pikv_prompt_attn, pikv_prompt_mass, pikv_prompt_mass_workspace_bytes,
+    pikv_paged_append, pikv_paged_attn, pikv_paged_attn_workspace_bytes, pikv_paged_fill,
     COMBINE_LOCAL, COMBINE_LSE, PENALTY_CACHE_AWARE, PENALTY_LOAD_BALANCE, PENALTY_ENTROPY, DESC_8BIT, DESC_VALUE_BIAS, PikvRouterFeedback,
     make_router_feedback, POLICY_H2O, POLICY_LRU,
     POLICY_LRU_PLUS, POLICY_SL, PikvDesc, PikvError, PikvPolicyArgs, make_policy_args, pikv_decode_step_policy, library_path, load_library, make_desc,

@@ -33,7 +33,8 @@ EXPORTS = ("pikv_route", "pikv_attn_workspace_bytes", "pikv_sharded_attn", "pikv
            "pikv_set_profile_events", "pikv_router_penalty", "pikv_compress", "pikv_policy_stamp",
            "pikv_update_utility_tracked", "pikv_policy_utility", "pikv_policy_compact", "pikv_decode_step_policy", "pikv_route_round_robin",
            "pikv_sharded_attn_noalloc", "pikv_norm_rope", "pikv_quant_pack", "pikv_quant_read", "pikv_quant_append",
-           "pikv_quant_attn_workspace_bytes", "pikv_quant_attn")
+           "pikv_quant_attn_workspace_bytes", "pikv_quant_attn", "pikv_prompt_attn", "pikv_prompt_mass_workspace_bytes", "pikv_prompt_mass",
+           "pikv_paged_fill", "pikv_paged_append", "pikv_paged_attn_workspace_bytes", "pikv_paged_attn")
 
 
 class PikvError(RuntimeError):
@@ -140,6 +141,23 @@ def load_library():
     lib.pikv_quant_attn.argtypes = [dp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, f32,
                                     vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     lib.pikv_quant_attn.restype = C.c_int
+    lib.pikv_prompt_attn.argtypes = [vp, vp, vp, i32, i64, i64, i64, i32, i32, i32, i32, vp, i32, i32, vp, f32, f32, vp, i32, vp, vp, vp, vp]
+    lib.pikv_prompt_attn.restype = C.c_int
+    lib.pikv_prompt_mass_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.pikv_prompt_mass_workspace_bytes.restype = C.c_size_t
+    lib.pikv_prompt_mass.argtypes = [vp, vp, i32, i64, i64, i32, i32, i32, i32, vp, i32, i32, vp, f32, f32, vp, i32, vp, vp, vp, vp,
+                                     C.c_size_t, vp]
+    lib.pikv_prompt_mass.restype = C.c_int
+    pp = C.POINTER(PikvPages)
+    lib.pikv_paged_fill.argtypes = [dp, pp, vp, vp, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.pikv_paged_fill.restype = C.c_int
+    lib.pikv_paged_append.argtypes = [dp, pp, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.pikv_paged_append.restype = C.c_int
+    lib.pikv_paged_attn_workspace_bytes.argtypes = [dp, i32]
+    lib.pikv_paged_attn_workspace_bytes.restype = C.c_size_t
+    lib.pikv_paged_attn.argtypes = [dp, pp, vp, vp, vp, vp, vp, vp, vp, i32, i32, f32, f32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                    C.c_size_t, vp]
+    lib.pikv_paged_attn.restype = C.c_int
     lib.pikv_version.argtypes = []
     lib.pikv_version.restype = C.c_int
     native = _load_native({name: C.cast(getattr(lib, name), C.c_void_p).value for name in EXPORTS})
@@ -165,7 +183,7 @@ def _load_native(addresses):
         warnings.warn("calls go through ctypes: _pikv_native.so is not built for this Python and torch (%s); "
                       "run `python -m paper_2508_06526_amd.build`" % e, RuntimeWarning, stacklevel=3)
         return _NoExtension()
-    native.setup(PikvDesc, PikvPolicyArgs, PikvRouterFeedback, addresses, _MARK)
+    native.setup(PikvDesc, PikvPolicyArgs, PikvRouterFeedback, PikvPages, addresses, _MARK)
     return native
 
 
@@ -685,5 +703,165 @@ def pikv_quant_attn(desc, format, block, q, K_shards, V_shards, K_scales, V_scal
             _p(gates), k, combine, float(scale), _p(y), _p(row_max), _p(row_norm), _p(scores), _p(slot_coef), _p(workspace), ws_bytes,
             s), stream, _attn_tensors(desc, block, q, K_shards, V_shards, K_scales, V_scales, n_valid, topk_idx, gates, k, y, row_max,
                                       row_norm, scores, slot_coef, workspace))
+    if st != 0:
+        _check(st, where)
+
+
+# ---- Between a prompt and a paged cache (checked as the calls above).
+class PikvPages(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("page", C.c_int32), ("stride_page", C.c_int64), ("stride_h", C.c_int64), ("stride_s", C.c_int64)]
+
+
+def make_pages(n_pages, page, Hkv, D, stride_page=None, stride_h=None, stride_s=None) -> PikvPages:
+    """Geometry of pools [n_pages, Hkv, page, D], or with strides (elements) of others: a pool of one tensor [n_pages, 2, Hkv, page, D]
+    for K and V has stride_page = 2 * Hkv * page * D, pages [n_pages, page, Hkv, D] have stride_h = D, stride_s = Hkv * D."""
+    if stride_s is None:
+        stride_s = D
+    if stride_h is None:
+        stride_h = page * stride_s
+    if stride_page is None:
+        stride_page = max(Hkv * stride_h, page * stride_s)
+    return PikvPages(n_pages, page, stride_page, stride_h, stride_s)
+
+
+def _pool(where, pool, desc, pages):
+    """Device address of a pool, which may be a part of a larger tensor: what lies behind it has to hold the pages."""
+    if pool is None:
+        return None
+    if not pool.is_cuda:
+        raise ValueError("libpikv takes device memory only")
+    extent = (pages.n_pages - 1) * pages.stride_page + (desc.Hkv - 1) * pages.stride_h + (pages.page - 1) * pages.stride_s + desc.D
+    held = pool.untyped_storage().nbytes() // pool.element_size() - pool.storage_offset()
+    if pool.is_contiguous():
+        held = min(held, pool.numel())
+    if desc.B > 0 and held < extent:
+        raise ValueError("%s: a pool holds %d elements, its pages take %d" % (where, held, extent))
+    if pool.dim() > 0 and pool.shape[-1] > 1 and pool.stride(-1) != 1:
+        raise ValueError("the values of a row must be contiguous")
+    return pool.data_ptr()
+
+
+def _paged_tensors(desc, pages, page_table, n_valid, entry_pos):
+    be = desc.B * desc.E
+    per_shard = (desc.S - 1) // pages.page + 1 if pages.page > 0 else 0
+    return [("page_table", page_table, be * per_shard), ("n_valid", n_valid, be), ("entry_pos", entry_pos, be * desc.S)]
+
+
+def _prompt_tensors(q, k, v, tokens, q_stride, k_stride, v_stride, Hq, Hkv, D, cu_seqlens, B, prefix, slopes, row_max, row_norm):
+    def rows(name, x, stride, heads):
+        if x is None:
+            return (name, x, 0)
+        if x.is_contiguous():
+            return (name, x, (tokens - 1) * stride + heads * D if tokens > 0 else 0)
+        return (name, x, max(tokens * x[:1].numel(), x.shape[0] * heads * D if tokens > 0 else 0))
+    return [rows("q", q, q_stride, Hq), rows("k", k, k_stride, Hkv), rows("v", v, v_stride, Hkv), ("cu_seqlens", cu_seqlens, B + 1),
+            ("prefix", prefix, B), ("slopes", slopes, Hq), ("row_max", row_max, tokens * Hq), ("row_norm", row_norm, tokens * Hq)]
+
+
+def pikv_prompt_attn(q, k, v, tokens, q_stride, k_stride, v_stride, Hq, Hkv, D, cu_seqlens, B, max_len, prefix, scale, cap, slopes, window,
+                     out, row_max=None, row_norm=None, stream=None):
+    """``q``, ``k``, ``v``: [tokens, heads * D] or [tokens, heads, D], rows ``*_stride`` elements apart (views into a wider projection are
+    taken as they are)."""
+    where = "pikv_prompt_attn"
+    st = _calls().pikv_prompt_attn(q, k, v, tokens, q_stride, k_stride, v_stride, Hq, Hkv, D, cu_seqlens, B, max_len, prefix, scale, cap,
+                                   slopes, window, out, row_max, row_norm, _raw(stream))
+    if st is None:
+        _typed(where, q.dtype, k, v, out)
+        _int32_float32(where, [cu_seqlens, prefix], [slopes, row_max, row_norm])
+        st = _on_device(where, lambda s: load_library().pikv_prompt_attn(
+            _rows(q, q_stride), _rows(k, k_stride), _rows(v, v_stride), tokens, q_stride, k_stride, v_stride, Hq, Hkv, D, _dtype_code(q),
+            _p(cu_seqlens), B, max_len, _p(prefix), float(scale), float(cap), _p(slopes), window, _p(out), _p(row_max), _p(row_norm), s),
+            stream, _prompt_tensors(q, k, v, tokens, q_stride, k_stride, v_stride, Hq, Hkv, D, cu_seqlens, B, prefix, slopes, row_max,
+                                    row_norm) + [("out", out, tokens * Hq * D)])
+    if st != 0:
+        _check(st, where)
+
+
+def pikv_prompt_mass_workspace_bytes(tokens, Hkv, B, max_len) -> int:
+    return int(load_library().pikv_prompt_mass_workspace_bytes(tokens, Hkv, B, max_len))
+
+
+def pikv_prompt_mass(q, k, tokens, q_stride, k_stride, Hq, Hkv, D, cu_seqlens, B, max_len, prefix, scale, cap, slopes, window, row_max,
+                     row_norm, mass, workspace, stream=None):
+    where = "pikv_prompt_mass"
+    st = _calls().pikv_prompt_mass(q, k, tokens, q_stride, k_stride, Hq, Hkv, D, cu_seqlens, B, max_len, prefix, scale, cap, slopes, window,
+                                   row_max, row_norm, mass, workspace, _raw(stream))
+    if st is None:
+        _typed(where, q.dtype, k)
+        _int32_float32(where, [cu_seqlens, prefix], [slopes, row_max, row_norm, mass])
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        st = _on_device(where, lambda s: load_library().pikv_prompt_mass(
+            _rows(q, q_stride), _rows(k, k_stride), tokens, q_stride, k_stride, Hq, Hkv, D, _dtype_code(q), _p(cu_seqlens), B, max_len,
+            _p(prefix), float(scale), float(cap), _p(slopes), window, _p(row_max), _p(row_norm), _p(mass), _p(workspace), ws_bytes, s),
+            stream, _prompt_tensors(q, k, None, tokens, q_stride, k_stride, 0, Hq, Hkv, D, cu_seqlens, B, prefix, slopes, row_max,
+                                    row_norm) + [("mass", mass, tokens), ("workspace", workspace, 0)])
+    if st != 0:
+        _check(st, where)
+
+
+def pikv_paged_fill(desc, pages, K_new, V_new, tokens, cu_seqlens, topk_idx, k, weight, positions, K_pool, V_pool, page_table, entry_pos,
+                    utility, n_valid, slots, stream=None):
+    where = "pikv_paged_fill"
+    st = _calls().pikv_paged_fill(desc, pages, K_new, V_new, tokens, cu_seqlens, topk_idx, k, weight, positions, K_pool, V_pool, page_table,
+                                  entry_pos, utility, n_valid, slots, _raw(stream))
+    if st is None:
+        _typed(where, _storage(desc), K_new, V_new, K_pool, V_pool)
+        _int32_float32(where, [cu_seqlens, topk_idx, positions, page_table, entry_pos, n_valid, slots], [weight, utility])
+        row = desc.Hkv * desc.D
+        st = _on_device(where, lambda s: load_library().pikv_paged_fill(
+            C.byref(desc), C.byref(pages), _p(K_new), _p(V_new), tokens, _p(cu_seqlens), _p(topk_idx), k, _p(weight), _p(positions),
+            _pool(where, K_pool, desc, pages), _pool(where, V_pool, desc, pages), _p(page_table), _p(entry_pos), _p(utility), _p(n_valid),
+            _p(slots), s), stream, _paged_tensors(desc, pages, page_table, n_valid, entry_pos) + [
+                ("K_new", K_new, tokens * row), ("V_new", V_new, tokens * row), ("cu_seqlens", cu_seqlens, desc.B + 1),
+                ("topk_idx", topk_idx, tokens * k), ("weight", weight, tokens), ("positions", positions, tokens), ("K_pool", K_pool, 0),
+                ("V_pool", V_pool, 0), ("utility", utility, desc.B * desc.E * desc.S), ("slots", slots, tokens * k)])
+    if st != 0:
+        _check(st, where)
+
+
+def pikv_paged_append(desc, pages, K_new, V_new, topk_idx, k, reuse_idx, reuse_cnt, max_evict, positions, K_pool, V_pool, page_table, entry_pos,
+                      utility, n_valid, stream=None):
+    where = "pikv_paged_append"
+    st = _calls().pikv_paged_append(desc, pages, K_new, V_new, topk_idx, k, reuse_idx, reuse_cnt, max_evict, positions, K_pool, V_pool,
+                                    page_table, entry_pos, utility, n_valid, _raw(stream))
+    if st is None:
+        _typed(where, _storage(desc), K_new, V_new, K_pool, V_pool)
+        _int32_float32(where, [topk_idx, reuse_idx, reuse_cnt, positions, page_table, entry_pos, n_valid], [utility])
+        row, be = desc.B * desc.Hkv * desc.D, desc.B * desc.E
+        st = _on_device(where, lambda s: load_library().pikv_paged_append(
+            C.byref(desc), C.byref(pages), _p(K_new), _p(V_new), _p(topk_idx), k, _p(reuse_idx), _p(reuse_cnt), max_evict, _p(positions),
+            _pool(where, K_pool, desc, pages), _pool(where, V_pool, desc, pages), _p(page_table), _p(entry_pos), _p(utility), _p(n_valid), s),
+            stream, _paged_tensors(desc, pages, page_table, n_valid, entry_pos) + [
+                ("K_new", K_new, row), ("V_new", V_new, row), ("topk_idx", topk_idx, desc.B * k), ("reuse_idx", reuse_idx, be * max_evict),
+                ("reuse_cnt", reuse_cnt, be), ("positions", positions, desc.B), ("K_pool", K_pool, 0), ("V_pool", V_pool, 0),
+                ("utility", utility, be * desc.S)])
+    if st != 0:
+        _check(st, where)
+
+
+def pikv_paged_attn_workspace_bytes(desc: PikvDesc, k: int) -> int:
+    return int(load_library().pikv_paged_attn_workspace_bytes(C.byref(desc), k))
+
+
+def pikv_paged_attn(desc, pages, q, K_pool, V_pool, page_table, n_valid, topk_idx, gates, k, combine, scale, cap, slopes, window, prefix,
+                    entry_pos, q_pos, y, row_max, row_norm, scores, slot_coef, workspace, stream=None):
+    where = "pikv_paged_attn"
+    st = _calls().pikv_paged_attn(desc, pages, q, K_pool, V_pool, page_table, n_valid, topk_idx, gates, k, combine, scale, cap, slopes, window,
+                                  prefix, entry_pos, q_pos, y, row_max, row_norm, scores, slot_coef, workspace, _raw(stream))
+    if st is None:
+        _typed(where, _storage(desc), q, K_pool, V_pool)
+        _int32_float32(where, [page_table, n_valid, topk_idx, prefix, entry_pos, q_pos], [gates, slopes, y, row_max, row_norm, scores, slot_coef])
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        heads, tq = desc.B * desc.Hq, max(desc.tq, 1)
+        selected = desc.B * desc.route_rows_per_seq * k
+        st = _on_device(where, lambda s: load_library().pikv_paged_attn(
+            C.byref(desc), C.byref(pages), _p(q), _pool(where, K_pool, desc, pages), _pool(where, V_pool, desc, pages), _p(page_table),
+            _p(n_valid), _p(topk_idx), _p(gates), k, combine, float(scale), float(cap), _p(slopes), window, _p(prefix), _p(entry_pos), _p(q_pos),
+            _p(y), _p(row_max), _p(row_norm), _p(scores), _p(slot_coef), _p(workspace), ws_bytes, s), stream,
+            _paged_tensors(desc, pages, page_table, n_valid, entry_pos) + [
+                ("q", q, heads * desc.D), ("K_pool", K_pool, 0), ("V_pool", V_pool, 0), ("topk_idx", topk_idx, selected), ("gates", gates, selected),
+                ("slopes", slopes, desc.Hq // tq), ("prefix", prefix, desc.B), ("q_pos", q_pos, desc.B * tq), ("y", y, heads * desc.D),
+                ("row_max", row_max, heads), ("row_norm", row_norm, heads), ("scores", scores, heads * k * desc.S, desc.S),
+                ("slot_coef", slot_coef, heads * k * 2), ("workspace", workspace, 0)])
     if st != 0:
         _check(st, where)

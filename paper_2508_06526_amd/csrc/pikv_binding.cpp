@@ -24,7 +24,7 @@
 namespace {
 
 // The classes of binding.py's ctypes structures; set once by setup(), which the binding calls when it loads the library.
-PyTypeObject *desc_type = nullptr, *policy_type = nullptr, *feedback_type = nullptr;
+PyTypeObject *desc_type = nullptr, *policy_type = nullptr, *feedback_type = nullptr, *pages_type = nullptr;
 
 // What shard_table marks tables of 8-bit shards with: only the calls on such shards take them.
 PyObject *eight_bit_mark = nullptr;
@@ -36,7 +36,8 @@ bool of_eight_bits(PyObject *tensor) {
 // Addresses of the library's functions, in the order of `Functions`.
 enum Function {
     kRoute, kAttn, kAttnNoalloc, kUtility, kUtilityTracked, kEvict, kAppend, kStep, kStepPolicy, kCompress, kStamp, kPolicyUtility,
-    kPolicyCompact, kPenalty, kNormRope, kQuantPack, kQuantRead, kQuantAppend, kQuantAttn, kFunctions
+    kPolicyCompact, kPenalty, kNormRope, kQuantPack, kQuantRead, kQuantAppend, kQuantAttn, kPromptAttn, kPromptMass, kPagedFill, kPagedAppend,
+    kPagedAttn, kFunctions
 };
 void *addresses[kFunctions] = {};
 
@@ -66,7 +67,7 @@ struct Args {
     at::ScalarType dense = at::ScalarType::Undefined;      // strict: the type of Dense tensors, the descriptor's or the first one's
     bool strict = false;                 // the tensors of int32_t *, float * and tables are of that type (tables: int64), and all are on one device
     // strict: what the tensor at each place holds, and its last dimension if it has four; a tensor that is not given holds anything
-    static constexpr int kPlaces = 20;
+    static constexpr int kPlaces = 24;
     int64_t held[kPlaces], last_of_four[kPlaces];
 
     template <typename T>
@@ -110,6 +111,8 @@ struct Take {
             T desc = Py_TYPE(o) == desc_type ? a.template buffer<T>(o) : a.template unusual<T>();
             if (desc != nullptr) a.dense = desc->dtype == PIKV_F32 ? at::kFloat : at::kBFloat16;
             return desc;
+        } else if constexpr (std::is_same_v<T, const pikv_pages *>) {
+            return Py_TYPE(o) == pages_type ? a.template buffer<T>(o) : a.template unusual<T>();
         } else if constexpr (std::is_same_v<T, const pikv_policy_args *> || std::is_same_v<T, const pikv_router_feedback *>) {
             if (o == Py_None) return nullptr;
             const bool mine = Py_TYPE(o) == (std::is_same_v<T, const pikv_policy_args *> ? policy_type : feedback_type);
@@ -247,6 +250,42 @@ bool all_hold(const Args &a, const VALUES &v) {
                    (a.last_of_four[17] < 0 || a.last_of_four[17] == d.S) && holds(18, heads * k * 2);
         }
     }
+    if constexpr (F == kPromptAttn || F == kPromptMass) {
+        constexpr int V = F == kPromptAttn ? 1 : 0;                  // (arguments of v in front of what both take)
+        const Count tokens = std::get<2 + V>(v), q_stride = std::get<3 + V>(v), k_stride = std::get<4 + V>(v), Hq = std::get<5 + 2 * V>(v),
+                    Hkv = std::get<6 + 2 * V>(v), D = std::get<7 + 2 * V>(v), B = std::get<10 + 2 * V>(v);
+        auto rows = [&](int place, Count stride, Count heads) { return holds(place, tokens > 0 ? (tokens - 1) * stride + heads * D : 0); };
+        if (!rows(0, q_stride, Hq) || !rows(1, k_stride, Hkv)) return false;
+        if constexpr (F == kPromptAttn)
+            return rows(2, std::get<6>(v), Hkv) && holds(10, B + 1) && holds(13, B) && holds(16, Hq) && holds(18, tokens * Hq * D) &&
+                   holds(19, tokens * Hq) && holds(20, tokens * Hq);
+        else
+            return holds(8, B + 1) && holds(11, B) && holds(14, Hq) && holds(16, tokens * Hq) && holds(17, tokens * Hq) && holds(18, tokens);
+    } else if constexpr (F == kPagedFill || F == kPagedAppend || F == kPagedAttn) {
+        const pikv_desc &d = *std::get<0>(v);
+        const pikv_pages &g = *std::get<1>(v);
+        const Count be = (Count)d.B * d.E, row = (Count)d.Hkv * d.D, extent = d.B > 0 ? (Count)(g.n_pages - 1) * g.stride_page +
+            (Count)(d.Hkv - 1) * g.stride_h + (Count)(g.page - 1) * g.stride_s + d.D : 0;
+        const Count table = g.page > 0 ? be * ((d.S - 1) / g.page + 1) : 0;
+        if constexpr (F == kPagedFill) {
+            const Count tokens = std::get<4>(v), k = std::get<7>(v);
+            return holds(2, tokens * row) && holds(3, tokens * row) && holds(5, (Count)d.B + 1) && holds(6, tokens * k) && holds(8, tokens) &&
+                   holds(9, tokens) && holds(10, extent) && holds(11, extent) && holds(12, table) && holds(13, be * d.S) && holds(14, be * d.S) &&
+                   holds(15, be) && holds(16, tokens * k);
+        }
+        if constexpr (F == kPagedAppend) {
+            const Count k = std::get<5>(v), max_evict = std::get<8>(v);
+            return holds(2, d.B * row) && holds(3, d.B * row) && holds(4, d.B * k) && holds(6, be * max_evict) && holds(7, be) && holds(9, d.B) &&
+                   holds(10, extent) && holds(11, extent) && holds(12, table) && holds(13, be * d.S) && holds(14, be * d.S) && holds(15, be);
+        }
+        if constexpr (F == kPagedAttn) {
+            const Count heads = (Count)d.B * d.Hq, k = std::get<9>(v), selected = (Count)d.B * d.route_rows_per_seq * k, tq = d.tq > 1 ? d.tq : 1;
+            return holds(2, heads * d.D) && holds(3, extent) && holds(4, extent) && holds(5, table) && holds(6, be) && holds(7, selected) &&
+                   holds(8, selected) && holds(13, d.Hq / tq) && holds(15, d.B) && holds(16, be * d.S) && holds(17, d.B * tq) &&
+                   holds(18, heads * d.D) && holds(19, heads) && holds(20, heads) && holds(21, heads * k * d.S) &&
+                   (a.last_of_four[21] < 0 || a.last_of_four[21] == d.S) && holds(22, heads * k * 2);
+        }
+    }
     return true;
 }
 
@@ -294,7 +333,7 @@ PyMethodDef method(const char *name) {
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&Caller<F, FN, KINDS...>::call)), METH_FASTCALL, nullptr};
 }
 
-// setup(descriptor class, policy class, feedback class, {name: address}, attribute of tables of 8-bit shards)
+// setup(descriptor class, policy class, feedback class, pages class, {name: address}, attribute of tables of 8-bit shards)
 PyObject *setup(PyObject *, PyObject *args);
 
 PyMethodDef methods[] = {
@@ -321,13 +360,22 @@ PyMethodDef methods[] = {
         "pikv_quant_append"),
     method<kQuantAttn, decltype(&pikv_quant_attn), At<3, Dense>, At<4, Codes>, At<5, Codes>, At<20, Bytes>, At<21, DeviceStream>>(
         "pikv_quant_attn"),
+    method<kPromptAttn, decltype(&pikv_prompt_attn), At<0, Dense>, At<1, Dense>, At<2, Dense>, At<10, Dtype>, At<19, Dense>,
+           At<22, DeviceStream>>("pikv_prompt_attn"),
+    method<kPromptMass, decltype(&pikv_prompt_mass), At<0, Dense>, At<1, Dense>, At<8, Dtype>, At<21, Bytes>, At<22, DeviceStream>>(
+        "pikv_prompt_mass"),
+    method<kPagedFill, decltype(&pikv_paged_fill), At<2, Dense>, At<3, Dense>, At<10, Dense>, At<11, Dense>, At<17, DeviceStream>>("pikv_paged_fill"),
+    method<kPagedAppend, decltype(&pikv_paged_append), At<2, Dense>, At<3, Dense>, At<10, Dense>, At<11, Dense>, At<16, DeviceStream>>(
+        "pikv_paged_append"),
+    method<kPagedAttn, decltype(&pikv_paged_attn), At<2, Dense>, At<3, Dense>, At<4, Dense>, At<24, Bytes>, At<25, DeviceStream>>("pikv_paged_attn"),
     {nullptr, nullptr, 0, nullptr},
 };
 
 PyObject *setup(PyObject *, PyObject *args) {
-    PyObject *desc, *policy, *feedback, *table;
+    PyObject *desc, *policy, *feedback, *pages, *table;
     const char *mark;
-    if (!PyArg_ParseTuple(args, "O!O!O!O!s", &PyType_Type, &desc, &PyType_Type, &policy, &PyType_Type, &feedback, &PyDict_Type, &table, &mark))
+    if (!PyArg_ParseTuple(args, "O!O!O!O!O!s", &PyType_Type, &desc, &PyType_Type, &policy, &PyType_Type, &feedback, &PyType_Type, &pages,
+                          &PyDict_Type, &table, &mark))
         return nullptr;
     if ((eight_bit_mark = PyUnicode_InternFromString(mark)) == nullptr) return nullptr;
     for (int f = 0; f < kFunctions; ++f) {
@@ -336,10 +384,11 @@ PyObject *setup(PyObject *, PyObject *args) {
         addresses[f] = PyLong_AsVoidPtr(address);
         if (PyErr_Occurred()) return nullptr;
     }
-    Py_INCREF(desc), Py_INCREF(policy), Py_INCREF(feedback);     // for the life of the process
+    Py_INCREF(desc), Py_INCREF(policy), Py_INCREF(feedback), Py_INCREF(pages);     // for the life of the process
     desc_type = reinterpret_cast<PyTypeObject *>(desc);
     policy_type = reinterpret_cast<PyTypeObject *>(policy);
     feedback_type = reinterpret_cast<PyTypeObject *>(feedback);
+    pages_type = reinterpret_cast<PyTypeObject *>(pages);
     Py_RETURN_NONE;
 }
 
