@@ -10,12 +10,13 @@
 //   * O^T[d][row] += V^T . P^T.
 // One pass with the running maximum and sum of the softmax (fp32).  bf16: a weight is rounded once, to bf16, on its way into the second
 // product - half a step of 2^-8 of each, as the output's own rounding - the sum is of the unrounded ones.
+#include "pikv_decode_dev.h"
 #include "pikv_prompt_dev.h"
 
 namespace pikv {
 namespace {
 
-constexpr int kWaves = 4, kThreads = kWaves * kWave, kRows = 32;      // rows of a wave
+constexpr int kWaves = 4, kThreads = kWaves * kWave, kWaveRows = 32;      // rows of a wave
 
 // LDS tiles of KEYS entries x D values, in 16-byte chunks, a row's chunks exchanged by an xor so that the reads of a wave spread over
 // the banks: K is read as one chunk of 32 entries each, V (bf16) as 64 bytes of 4 neighbouring entries each.
@@ -38,15 +39,13 @@ __device__ __forceinline__ uint2 read_transposed(const void *at) {
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)at));
 }
 
-__device__ __forceinline__ bool not_finite(float x) { return !(x - x == 0.0f); }
-
-template <typename T, int D, bool CHANGED>
+// CAP: scores capped by a tanh; BIAS: with a distance term.
+template <typename T, int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
     typedef Tile<T, D> L;
     constexpr bool BF = sizeof(T) == 2;
     constexpr int KEYS = L::KEYS, KB = KEYS / 32, DT = D / 32, BUFFERS = 2;
     constexpr int QN = D * (int)sizeof(T) / 32;                       // 16-byte pieces of a lane's query
-    constexpr float kLog2e = 1.44269504088896340736f;
     __shared__ __attribute__((aligned(16))) uint4 Ks[BUFFERS][KEYS * L::CHUNKS], Vs[BUFFERS][KEYS * L::CHUNKS];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, h = lane >> 5;
@@ -67,32 +66,71 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
     auto after = [&](int t) { return t + 1 < prefix_tiles ? t + 1 : max(t + 1, window_tile); };
 
     // the wave's rows
-    const int wave_row = row0 + wave * kRows;
+    const int wave_row = row0 + wave * kWaveRows;
     const int row = min(wave_row + c, rows - 1), token = row_token(p, row), head = hk * p.G + row - token * p.G;
-    const int wave_first = row_token(p, min(wave_row, rows - 1)), wave_last = row_token(p, min(wave_row + kRows, rows) - 1);
-    const float slope = CHANGED && p.slopes ? p.slopes[head] : 0.0f;
+    const int wave_first = row_token(p, min(wave_row, rows - 1)), wave_last = row_token(p, min(wave_row + kWaveRows, rows) - 1);
+    // Scores are kept as they come: products (capped: parts of the cap) that p.unit makes scores of, or with a distance term scores.
+    const float to_log2 = p.unit_log2, slope = BIAS ? p.slopes[head] : 0.0f;
 
-    const char *Kb = static_cast<const char *>(p.k) + ((int64_t)span.first * p.k_stride + hk * D) * sizeof(T);
-    const char *Vb = static_cast<const char *>(p.v) + ((int64_t)span.first * p.v_stride + hk * D) * sizeof(T);
-    uint4 kr[L::PER_THREAD], vr[L::PER_THREAD];
-    auto request = [&](int t) {
-#pragma unroll
-        for (int u = 0; u < L::PER_THREAD; ++u) {
-            const int at = tid + u * kThreads, key = min(t * KEYS + at / L::CHUNKS, n - 1), chunk = at % L::CHUNKS;      // (past the end: the last entry again)
-            kr[u] = load16(Kb + (int64_t)key * p.k_stride * sizeof(T) + chunk * 16);
-            vr[u] = load16(Vb + (int64_t)key * p.v_stride * sizeof(T) + chunk * 16);
-        }
+    const int64_t k_bytes = p.k_stride * (int64_t)sizeof(T), v_bytes = p.v_stride * (int64_t)sizeof(T);
+    const char *Kb = static_cast<const char *>(p.k) + span.first * k_bytes + hk * D * (int)sizeof(T);
+    const char *Vb = static_cast<const char *>(p.v) + span.first * v_bytes + hk * D * (int)sizeof(T);
+    auto opaque = [](uint32_t v) {           // (else an address per read is carried through the loop)
+        asm volatile("" : "+v"(v));
+        return v;
     };
-    auto place = [&](int buffer) {
+    uint32_t kr[L::PER_THREAD][4], vr[L::PER_THREAD][4];
+    // A tile's rows; those past the end read as zeros.
+    auto request = [&](uint32_t (&to)[L::PER_THREAD][4], const char *base, int64_t stride, int t) {
+        const int here = min(n - t * KEYS, KEYS);
+        const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + t * KEYS * stride), 0, (uint32_t)(here - 1) * (uint32_t)stride + D * (int)sizeof(T), 0x00020000);
+        const uint32_t at = opaque((tid / L::CHUNKS) * (uint32_t)stride + (tid % L::CHUNKS) * 16);
 #pragma unroll
-        for (int u = 0; u < L::PER_THREAD; ++u) {
-            const int at = tid + u * kThreads, key = at / L::CHUNKS, chunk = at % L::CHUNKS;
-            Ks[buffer][L::k_chunk(key, chunk)] = kr[u];
-            Vs[buffer][L::v_chunk(key, chunk)] = vr[u];
+        for (int u = 0; u < L::PER_THREAD; ++u) buffer_load<16, false>(to[u], from, at + u * (kThreads / L::CHUNKS) * (uint32_t)stride);
+    };
+    // Whether rows first .. last of tokens see all entries of a tile.
+    auto seen_whole = [&](int t, int first, int last) {
+        const int key0 = t * KEYS;
+        return key0 + KEYS <= n && (key0 + KEYS <= prefix || (key0 + KEYS - 1 <= first && (p.window <= 0 || last - key0 < p.window)));
+    };
+    // A value that is no number stays out of the rows that do not see its entry: 0 x NaN is NaN.  Where a tile is not seen whole such
+    // values go to LDS as zeros, and the block is told (rare).
+    auto place = [&](int t, int buffer) {
+        auto special = [](uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; };
+        bool bad = false;
+        if (!seen_whole(t, first_token, last_token)) {
+#pragma unroll
+            for (int u = 0; u < L::PER_THREAD; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bad |= special(vr[u][i]) || (BF && special(vr[u][i] << 16));
         }
+        // pieces tid, tid + kThreads, ..: whole lines further on (fp32 rows of 128 values: half the exchange's 16 rows)
+        constexpr int LINES = kThreads / L::CHUNKS;
+        const uint32_t to_k = opaque(L::k_chunk(tid / L::CHUNKS, tid % L::CHUNKS) * 16 + buffer * (int)sizeof(Ks[0]));
+        const uint32_t to_v = opaque(L::v_chunk(tid / L::CHUNKS, tid % L::CHUNKS) * 16 + buffer * (int)sizeof(Vs[0]));
+        auto write_v = [&](auto of) {
+#pragma unroll
+            for (int u = 0; u < L::PER_THREAD; ++u)
+                *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(Vs) + to_v + u * kThreads * 16) = make_uint4(of(vr[u][0]), of(vr[u][1]), of(vr[u][2]), of(vr[u][3]));
+        };
+#pragma unroll
+        for (int u = 0; u < L::PER_THREAD; ++u)
+            *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(Ks) + ((LINES == 8 ? to_k ^ (u % 2 * 128) : to_k) + u * kThreads * 16)) =
+                make_uint4(kr[u][0], kr[u][1], kr[u][2], kr[u][3]);
+        if (__any(bad))
+            write_v([&](uint32_t w) { return (special(w) ? 0u : w & (BF ? 0xffff0000u : 0xffffffffu)) | (BF && !special(w << 16) ? w & 0xffffu : 0u); });
+        else
+            write_v([](uint32_t w) { return w; });
+        return bad;
+    };
+    auto placed = [&](int t, bool bad) {         // the barrier behind it: whether the tile held any
+        if (!seen_whole(t, first_token, last_token)) return __syncthreads_or(bad) != 0;
+        __syncthreads();
+        return false;
     };
     int tile = prefix_tiles > 0 ? 0 : window_tile;
-    request(tile);
+    request(kr, Kb, k_bytes, tile);
+    request(vr, Vb, v_bytes, tile);
     // the query operand: 16-byte pieces 2 s + h of row c
     uint4 q[QN];
     {
@@ -105,18 +143,24 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
-    float m = -INFINITY, l = 0.0f;       // of the products (CHANGED: of the scores)
-    const float to_log2 = CHANGED ? kLog2e : p.scale * kLog2e;
-    place(0);
-    __syncthreads();
+    // The maximum of the lane's scores so far; what they are taken relative to, which follows it only when a weight would pass 2^8:
+    // most tiles then leave the accumulators alone.
+    float top = -INFINITY, base = -INFINITY, shift = 0.0f, l = 0.0f;        // shift: base, 0 while nothing has been seen
+    // accumulators that get an infinity at the end (a NaN: both), 32 to a word
+    constexpr int WORDS = (DT * 16 + 31) / 32;
+    uint32_t most_inf[WORDS] = {}, least_inf[WORDS] = {};
+    bool odd = placed(tile, place(tile, 0));
     int buffer = 0;
     for (; tile <= last_tile; buffer ^= 1) {
         const int next = after(tile), key0 = tile * KEYS;
-        if (next <= last_tile) request(next);
+        const int lane = (int)opaque(tid) & (kWave - 1), c = lane & 31, h = lane >> 5;      // (derived again in every round: registers)
+        if (next <= last_tile) request(kr, Kb, k_bytes, next);
         const bool in_prefix = key0 < prefix;
         const bool any = in_prefix || (key0 <= wave_last && (p.window <= 0 || wave_first - (key0 + KEYS - 1) < p.window));
         if (any) {
             float s[KB][16];
+            // chunk 2 u + h of entry c, exchanged: the exchange of chunk h with 2 u's bits on top
+            const uint32_t k_at = opaque(L::k_chunk(c, h) * 16 + buffer * (int)sizeof(Ks[0]));
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 f32x16_t sc;
@@ -124,7 +168,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
                 for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
 #pragma unroll
                 for (int u = 0; u < QN; ++u) {
-                    const uint4 kop = Ks[buffer][L::k_chunk(kb * 32 + c, 2 * u + h)];
+                    const uint4 kop = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(Ks) + ((k_at ^ (u * 32)) + kb * 32 * L::CHUNKS * 16));
                     if constexpr (BF) {
                         sc = mfma32(kop, q[u], sc);
                     } else {
@@ -136,20 +180,18 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[kb][i] = sc[i];
-                if constexpr (CHANGED) {
-                    if (p.cap > 0.0f) cap_scores(s[kb], p.scale, p.cap, p.cap_rcp);
-                    const float unit = p.cap > 0.0f ? 1.0f : p.scale;
+                if constexpr (CAP) cap_parts(s[kb], p.scale * p.cap_rcp);
+                if constexpr (BIAS) {
                     const int first = key0 + kb * 32 + 4 * h - token;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(-slope, fabsf((float)(first + 8 * (i >> 2) + (i & 3))), s[kb][i] * unit);
+                    for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(-slope, fabsf((float)(first + 8 * (i >> 2) + (i & 3))), s[kb][i] * (CAP ? p.cap : p.scale));
                 }
             }
-            // seen whole by all rows of the wave, or not
-            const bool masked = !(key0 + KEYS <= n && (key0 + KEYS <= prefix || (key0 + KEYS - 1 <= wave_first &&
-                                                                                (p.window <= 0 || wave_last - key0 < p.window))));
-            auto seen = [&](int key) {
-                return key < n && (key < prefix || (key <= token && (p.window <= 0 || token - key < p.window)));
-            };
+            if (next <= last_tile) request(vr, Vb, v_bytes, next);      // (behind the first product: its registers)
+            const bool masked = !seen_whole(tile, wave_first, wave_last);
+            // the lane's row sees entries low .. token and those below the prefix
+            const int low = p.window > 0 ? max(token - p.window + 1, 0) : 0;
+            auto seen = [&](int key) { return (uint32_t)(key - low) <= (uint32_t)(token - low) || key < prefix; };
             if (masked) {
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
@@ -162,11 +204,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) most = fmaxf(most, s[kb][i]);
-            const float now = fmaxf(m, halves_max(most));
-            const float base = now == -INFINITY ? 0.0f : now;        // (nothing seen yet: weights of zero)
-            if (__any(now > m)) {
-                const float corr = __builtin_amdgcn_exp2f((m - base) * to_log2);
-                m = now;
+            top = fmaxf(top, most);
+            if (__any(most > base + p.margin)) {
+                const float now = halves_max(fmaxf(top, base)), next_shift = now == -INFINITY ? 0.0f : now;
+                const float corr = __builtin_amdgcn_exp2f((base - next_shift) * to_log2);
+                base = now;
+                shift = next_shift;
                 l *= corr;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
@@ -174,31 +217,20 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
                     for (int i = 0; i < 16; ++i) acc[d][i] *= corr;
             }
             float sum = 0.0f;
+            const float shift_log2 = -shift * to_log2;
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    s[kb][i] = __builtin_amdgcn_exp2f((s[kb][i] - base) * to_log2);
+                    // (bf16: one rounding less to spare, one operation less)
+                    s[kb][i] = __builtin_amdgcn_exp2f(BF ? fmaf(s[kb][i], to_log2, shift_log2) : (s[kb][i] - shift) * to_log2);
                     sum += s[kb][i];
                 }
             l += sum;
-            // A value that is no number stays out of the rows that do not see its entry: 0 x NaN is NaN.  (Rare; found per tile.)
-            bool odd = false;
-            if (masked) {
-                uint32_t most_exponent = 0;
-                const uint32_t *words = reinterpret_cast<const uint32_t *>(Vs[buffer]);
-                for (int i = lane; i < KEYS * L::CHUNKS * 4; i += kWave) {
-                    const uint32_t w = words[i] & 0x7fffffffu;
-                    most_exponent = max(most_exponent, BF ? max(w >> 16, w & 0x7fffu) : w);
-                }
-                odd = __any(most_exponent >= (BF ? 0x7f80u : 0x7f800000u));
-            }
-            auto finite = [&](uint32_t w) {      // bf16: two values; those that are no numbers become zero
-                if constexpr (BF) return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
-                else return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
-            };
             if constexpr (BF) {
-                const char *Vt = reinterpret_cast<const char *>(Vs[buffer]);
+                // 16 lanes read 4 entries x 16 values: lane g of them entry g / 4, values 4 (g % 4) .. of the 16 (lane & 16 ..)
+                const int g = lane & 15, value = (lane & 16) + 4 * (g & 3);
+                const uint32_t v_at = opaque(L::v_chunk(4 * h + (g >> 2), value >> 3) * 16 + (value & 7) * 2 + buffer * (int)sizeof(Vs[0]));
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -207,11 +239,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
                         split_bf16(&s[kb][8 * st], pop);
 #pragma unroll
                         for (int d = 0; d < DT; ++d) {
-                            // 16 lanes read 4 entries x 16 values: lane g of them entry g / 4, values 4 (g % 4) ..
-                            const int g = lane & 15, key = kb * 32 + 16 * st + 4 * h + (g >> 2), value = d * 32 + (lane & 16) + 4 * (g & 3);
-                            uint2 lo = read_transposed(Vt + L::v_chunk(key, value >> 3) * 16 + (value & 7) * 2);
-                            uint2 hi = read_transposed(Vt + L::v_chunk(key + 8, value >> 3) * 16 + (value & 7) * 2);
-                            if (odd) lo = make_uint2(finite(lo.x), finite(lo.y)), hi = make_uint2(finite(hi.x), finite(hi.y));
+                            const char *at = reinterpret_cast<const char *>(Vs) + ((v_at ^ (d * 64)) + (kb * 32 + 16 * st) * L::CHUNKS * 16);
+                            const uint2 lo = read_transposed(at), hi = read_transposed(at + 8 * L::CHUNKS * 16);
                             acc[d] = mfma32(make_uint4(lo.x, lo.y, hi.x, hi.y), pop[0], acc[d]);
                         }
                     }
@@ -220,37 +249,46 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        float v = Vt[(8 * (i >> 2) + 4 * h + (i & 3)) * D + d * 32 + c];
-                        if (odd) v = __uint_as_float(finite(__float_as_uint(v)));
-                        acc[d] = mfma32(v, s[0][i], acc[d]);
-                    }
+                    for (int d = 0; d < DT; ++d) acc[d] = mfma32(Vt[(8 * (i >> 2) + 4 * h + (i & 3)) * D + d * 32 + c], s[0][i], acc[d]);
             }
             if (odd) {
-                for (int key = 0; key < KEYS; ++key) {
-                    if (!seen(key0 + key)) continue;
+                for (int key = key0; key < min(key0 + KEYS, n); ++key) {
+                    if (!seen(key)) continue;
+                    const T *row = reinterpret_cast<const T *>(Vb + key * v_bytes);
 #pragma unroll
-                    for (int d = 0; d < DT; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int value = d * 32 + 8 * (i >> 2) + 4 * h + (i & 3), per = 16 / (int)sizeof(T);
-                            const T *chunk = reinterpret_cast<const T *>(&Vs[buffer][L::v_chunk(key, value / per)]);
-                            const float v = load_scalar<T>(chunk, value % per);
-                            if (not_finite(v)) acc[d][i] += v;
-                        }
+                    for (int j = 0; j < DT * 16; ++j) {
+                        const float v = load_scalar<T>(row, (j >> 4) * 32 + 8 * (j >> 2 & 3) + 4 * h + (j & 3));
+                        most_inf[j / 32] |= v == INFINITY || v != v ? 1u << (j & 31) : 0u;
+                        least_inf[j / 32] |= v == -INFINITY || v != v ? 1u << (j & 31) : 0u;
+                        if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (all at once they cost registers of the whole loop)
+                    }
                 }
             }
         }
-        if (next <= last_tile) place(buffer ^ 1);
-        __syncthreads();
+        if (!any && next <= last_tile) request(vr, Vb, v_bytes, next);
+        odd = next <= last_tile && placed(next, place(next, buffer ^ 1));
         tile = next;
     }
+    bool any_inf = false;
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) any_inf |= (most_inf[w] | least_inf[w]) != 0u;
+    if (__any(any_inf)) {
+#pragma unroll
+        for (int j = 0; j < DT * 16; ++j) {
+            if (most_inf[j / 32] >> (j & 31) & 1u) acc[j >> 4][j & 15] += INFINITY;
+            if (least_inf[j / 32] >> (j & 31) & 1u) acc[j >> 4][j & 15] -= INFINITY;
+        }
+    }
     l = halves_sum(l);
-    if (wave_row + c >= rows) return;
-    const int64_t to = (int64_t)(span.first + token) * p.Hq + head;
-    if (p.row_max && h == 0) {
-        p.row_max[to] = CHANGED ? m : m * p.scale;
-        p.row_norm[to] = l;
+    top = halves_max(top);
+    // (found again: not carried through the loop)
+    const int my_lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), my_h = my_lane >> 5;
+    const int my_row = wave_row + (my_lane & 31), my_token = row_token(p, my_row);
+    if (my_row >= rows) return;
+    const int64_t to = (int64_t)(span.first + my_token) * p.Hq + hk * p.G + my_row - my_token * p.G;
+    if (p.row_max && my_h == 0) {
+        p.row_max[to] = top * p.unit;
+        p.row_norm[to] = l * __builtin_amdgcn_exp2f((shift - (top == -INFINITY ? 0.0f : top)) * to_log2);
     }
     const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;    // (a NaN stays one)
     T *out = static_cast<T *>(p.out) + to * D;
@@ -261,7 +299,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
             float v[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) v[x] = acc[d][4 * u + x] * inv;
-            T *at = out + d * 32 + 8 * u + 4 * h;
+            T *at = out + d * 32 + 8 * u + 4 * my_h;
             if constexpr (BF) {
                 uint2 packed[1];
                 split_bf16(v, packed);
@@ -293,6 +331,9 @@ extern "C" int pikv_prompt_attn(const void *q, const void *k, const void *v, int
     PromptParams p = prompt_params(q, k, tokens, q_stride, k_stride, Hq, Hkv, D, cu_seqlens, B, max_len, prefix, scale, cap, slopes, window);
     p.v = v;
     p.v_stride = v_stride;
+    p.unit = slopes ? 1.0f : cap > 0.0f ? cap : p.scale;
+    p.unit_log2 = p.unit * 1.44269504088896340736f;
+    p.margin = 8.0f / p.unit_log2;
     p.out = out;
     p.row_max = row_max;
     p.row_norm = row_norm;
@@ -304,8 +345,13 @@ extern "C" int pikv_prompt_attn(const void *q, const void *k, const void *v, int
     auto launch = [&](auto type, auto width) {
         typedef decltype(type) T;
         constexpr int W = decltype(width)::value;
-        if (cap > 0.0f || slopes) hipLaunchKernelGGL((prompt_attn<T, W, true>), grid, threads, 0, st, p);
-        else hipLaunchKernelGGL((prompt_attn<T, W, false>), grid, threads, 0, st, p);
+        if (cap > 0.0f) {
+            if (slopes) hipLaunchKernelGGL((prompt_attn<T, W, true, true>), grid, threads, 0, st, p);
+            else hipLaunchKernelGGL((prompt_attn<T, W, true, false>), grid, threads, 0, st, p);
+        } else {
+            if (slopes) hipLaunchKernelGGL((prompt_attn<T, W, false, true>), grid, threads, 0, st, p);
+            else hipLaunchKernelGGL((prompt_attn<T, W, false, false>), grid, threads, 0, st, p);
+        }
     };
     auto by_width = [&](auto type) {
         if (D == 32) launch(type, std::integral_constant<int, 32>{});

@@ -20,6 +20,7 @@ struct PromptParams {
     uint32_t G_rcp;                     // 2^32 / G, rounded up: a row of a kv head's queries / G
     int tokens, max_len, Hq, Hkv, G, B, window, tiles, nsplit;
     float scale, cap, cap_rcp;
+    float unit, unit_log2, margin;      // pikv_prompt_attn: of the scores as they are kept
 };
 
 // row / G for 0 <= row < 2^31 / G: rows of a kv head are (token, head of the group).
@@ -65,6 +66,8 @@ inline int check_prompt(const void *q, const void *k, const void *v, bool values
     auto rows = [&](const void *p, int64_t stride, int heads) {
         return stride >= (int64_t)heads * D && stride * es % 16 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
     };
+    // (64 rows are addressed with 32 bits)
+    if (q_stride * es > (1 << 25) || k_stride * es > (1 << 25) || (values && v_stride * es > (1 << 25))) return PIKV_ERR_UNSUPPORTED;
     if (!rows(q, q_stride, Hq) || !rows(k, k_stride, Hkv) || (values && !rows(v, v_stride, Hkv))) return PIKV_ERR_INVALID;
     return PIKV_OK;
 }
