@@ -298,7 +298,7 @@ __global__ __launch_bounds__(WAVES *kWave, WAVES == kWaves ? (RT == 1 && !(POS &
 #pragma unroll
                 for (int x = 0; x < NX; ++x) {
                     // (unsigned: a negative position lies beyond either)
-                    const bool sees = (uint32_t)pos[x] - (uint32_t)low[rt] < reach[rt] || (uint32_t)pos[x] < prefix;
+                    const bool sees = ((uint32_t)pos[x] - (uint32_t)low[rt] < reach[rt]) | ((uint32_t)pos[x] < prefix);
                     const int far = (int)((uint32_t)my_pos[rt] - (uint32_t)pos[x]);
                     sv[rt][x] = sees ? fmaf(-slope[rt], fabsf((float)far), sv[rt][x]) : -INFINITY;
                     seen[rt] |= sees ? 1u << x : 0u;

@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
             const bool masked = !seen_whole(tile, wave_first, wave_last);
             // the lane's row sees entries low .. token and those below the prefix
             const int low = p.window > 0 ? max(token - p.window + 1, 0) : 0;
-            auto seen = [&](int key) { return (uint32_t)(key - low) <= (uint32_t)(token - low) || key < prefix; };
+            auto seen = [&](int key) { return ((uint32_t)(key - low) <= (uint32_t)(token - low)) | (key < prefix); };
             if (masked) {
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)

@@ -1,10 +1,10 @@
 // The attention that each entry of a prompt got, over all of its tokens and query heads (Table 3 row H2O): column sums of the softmax, from
 // the rows' maxima and sums that the attention left.
 //
-//   mass_partial : a block takes 128 entries of a kv head, 32 a wave, their keys in registers, and walks the rows (token, head of
+//   mass_partial : a block takes 256 entries of a kv head, 64 a wave, their keys in registers, and walks the rows (token, head of
 //                  the group) that see any of them, 64 at a time through LDS.  S[row][entry] = Q . K^T puts an entry in a
-//                  lane: lane (c, h) = (lane % 32, lane / 32) gets entry c's scores of rows 8 (i / 4) + 4 h + i % 4 of each 32, and
-//                  sums exp(s - row_max) / row_norm in its own registers, 32 rows at a time and then over them.
+//                  lane: lane (c, h) = (lane % 32, lane / 32) gets the scores of entries c and 32 + c at rows 8 (i / 4) + 4 h + i % 4 of each 32,
+//                  and sums exp(s - row_max) / row_norm in its own registers, 32 rows at a time and then over them.
 //   mass_join    : the kv heads' sums (and those of the runs that few blocks' rows were cut into), in a fixed order.
 #include "pikv_prompt_dev.h"
 
@@ -12,7 +12,10 @@ namespace pikv {
 namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
-constexpr int kEntries = 32;             // of a wave
+// Entries of a wave, in 32 (fp32 keys of 64 would take all registers).
+template <typename T>
+constexpr int sets_of = sizeof(T) == 2 ? 2 : 1;
+constexpr int kMostEntries = kWaves * 32 * 2;        // of a block
 
 template <typename T, int D>
 struct QTile {
@@ -22,15 +25,16 @@ struct QTile {
     static __device__ __forceinline__ int chunk(int row, int c) { return row * CHUNKS + (c ^ ((row / PER_LINE) & (CHUNKS < 16 ? CHUNKS - 1 : 15))); }
 };
 
-template <typename T, int D, bool CHANGED>
+// CAP: scores capped by a tanh; BIAS: with a distance term.
+template <typename T, int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
     typedef QTile<T, D> L;
     constexpr bool BF = sizeof(T) == 2;
-    constexpr int ROWS = L::ROWS, KN = D * (int)sizeof(T) / 32;
+    constexpr int ROWS = L::ROWS, KN = D * (int)sizeof(T) / 32, SETS = sets_of<T>, ENTRIES = 32 * SETS;
     constexpr float kLog2e = 1.44269504088896340736f;
     __shared__ __attribute__((aligned(16))) uint4 Qs[2][ROWS * L::CHUNKS];
     // of a tile's rows: maximum, 1 / sum (0: gives nothing), token, slope
-    __shared__ __attribute__((aligned(16))) float row_max_s[2][ROWS], weight_s[2][ROWS], slope_s[2][CHANGED ? ROWS : 4];
+    __shared__ __attribute__((aligned(16))) float row_max_s[2][ROWS], weight_s[2][ROWS], slope_s[2][BIAS ? ROWS : 4];
     __shared__ __attribute__((aligned(16))) int token_s[2][ROWS];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, h = lane >> 5;
@@ -39,10 +43,10 @@ __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
     id = fast_divide(p.by_split, id, &split);
     const int at_tile = fast_divide(p.by_tile, id, &b);               // the entries with the most rows first
     const Span span = prompt_span(p, b);
-    const int n = span.n, entry0 = at_tile * kPromptTile;
+    const int n = span.n, entry0 = at_tile * kWaves * ENTRIES;
     if (entry0 >= n) return;
     const int prefix = p.prefix ? __builtin_amdgcn_readfirstlane(min(max(p.prefix[b], 0), n)) : 0;
-    const int entries_end = min(entry0 + kPromptTile, n);
+    const int entries_end = min(entry0 + kWaves * ENTRIES, n);
     // the rows that see any of the block's entries, and this block's run of them
     const bool all = entry0 < prefix;
     const int64_t seen_to = all || p.window <= 0 ? n : min((int64_t)n, (int64_t)entries_end - 1 + p.window);
@@ -50,21 +54,27 @@ __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
     const int per = ((row_hi - row_lo + p.nsplit - 1) / p.nsplit + ROWS - 1) / ROWS * ROWS;
     const int from = row_lo + split * per, to = min(row_hi, from + per);
 
-    const int wave_entry = entry0 + wave * kEntries, entry = wave_entry + c;
-    uint4 kop[KN];
-    {
-        const char *K = static_cast<const char *>(p.k) + ((int64_t)(span.first + min(entry, n - 1)) * p.k_stride + (int64_t)hk * D) * sizeof(T);
+    const int wave_entry = entry0 + wave * ENTRIES;
+    uint4 kop[SETS][KN];
 #pragma unroll
-        for (int s = 0; s < KN; ++s) kop[s] = load16(K + (2 * s + h) * 16);
+    for (int set = 0; set < SETS; ++set) {
+        const char *K = static_cast<const char *>(p.k) + ((int64_t)(span.first + min(wave_entry + 32 * set + c, n - 1)) * p.k_stride + (int64_t)hk * D) * sizeof(T);
+#pragma unroll
+        for (int s = 0; s < KN; ++s) kop[set][s] = load16(K + (2 * s + h) * 16);
     }
+    auto opaque = [](uint32_t v) {           // (else an address per read is carried through the loop)
+        asm volatile("" : "+v"(v));
+        return v;
+    };
     uint4 qr[L::PER_THREAD];
     float max_r = 0.0f, norm_r = 0.0f, slope_r = 0.0f;
     int token_r = 0;
     auto request = [&](int row0) {
+        const int tid = (int)opaque(threadIdx.x);
 #pragma unroll
         for (int u = 0; u < L::PER_THREAD; ++u) {
             const int at = tid + u * kThreads, row = min(row0 + at / L::CHUNKS, to - 1), token = row_token(p, row), head = hk * p.G + row - token * p.G;
-            qr[u] = load16(static_cast<const char *>(p.q) + ((int64_t)(span.first + token) * p.q_stride + (int64_t)head * D) * sizeof(T) + (at % L::CHUNKS) * 16);
+            qr[u] = load16(static_cast<const char *>(p.q) + ((int64_t)(span.first + token) * p.q_stride + head * D) * (int64_t)sizeof(T) + (at % L::CHUNKS) * 16);
         }
         if (tid < ROWS) {
             const int row = min(row0 + tid, to - 1), head = hk * p.G + row - row_token(p, row) * p.G;
@@ -72,10 +82,11 @@ __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
             const int64_t at = (int64_t)(span.first + token_r) * p.Hq + head;
             max_r = p.row_max[at];
             norm_r = row0 + tid < to ? p.row_norm[at] : 0.0f;
-            if (CHANGED && p.slopes) slope_r = p.slopes[head];
+            if constexpr (BIAS) slope_r = p.slopes[head];
         }
     };
     auto place = [&](int buffer) {
+        const int tid = (int)opaque(threadIdx.x);
 #pragma unroll
         for (int u = 0; u < L::PER_THREAD; ++u) {
             const int at = tid + u * kThreads;
@@ -85,117 +96,160 @@ __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
             row_max_s[buffer][tid] = norm_r == 0.0f ? INFINITY : max_r;
             weight_s[buffer][tid] = norm_r == 0.0f ? 0.0f : 1.0f / norm_r;
             token_s[buffer][tid] = token_r;
-            if constexpr (CHANGED) slope_s[buffer][tid] = slope_r;
+            if constexpr (BIAS) slope_s[buffer][tid] = slope_r;
         }
     };
-    float total = 0.0f;
+    float total[SETS] = {};
     if (from < to) {                             // (uniform)
         request(from);
         place(0);
         __syncthreads();
         int buffer = 0;
         for (int row0 = from; row0 < to; row0 += ROWS, buffer ^= 1) {
+            const int lane = (int)opaque(threadIdx.x) & (kWave - 1), c = lane & 31, h = lane >> 5;      // (derived again in every round: registers)
             if (row0 + ROWS < to) request(row0 + ROWS);
             const int first_token = row_token(p, row0), last_token = row_token(p, min(row0 + ROWS, to) - 1);
-            const bool any = wave_entry < n && (wave_entry < prefix || (wave_entry <= last_token && (p.window <= 0 || first_token - (wave_entry + kEntries - 1) < p.window)));
+            const bool any = wave_entry < n && (wave_entry < prefix || (wave_entry <= last_token && (p.window <= 0 || first_token - (wave_entry + ENTRIES - 1) < p.window)));
             if (any) {
-                const bool masked = !(wave_entry + kEntries <= prefix || (wave_entry + kEntries - 1 <= first_token &&
+                const bool masked = !(wave_entry + ENTRIES <= prefix || (wave_entry + ENTRIES - 1 <= first_token &&
                                                                           (p.window <= 0 || last_token - wave_entry < p.window))) || row0 + ROWS > to;
+                const uint32_t q_at = opaque(L::chunk(c, h) * 16 + buffer * (int)sizeof(Qs[0]));
+                const uint32_t reach = p.window > 0 ? p.window : 0x80000000u;
+                auto rows_of = [&](auto with_mask) {
+                    constexpr bool MASKED = decltype(with_mask)::value;
 #pragma unroll
-                for (int rb = 0; rb < ROWS / 32; ++rb) {
-                    f32x16_t sc;
+                    for (int rb = 0; rb < ROWS / 32; ++rb) {
+                        f32x16_t sc[SETS];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+                        for (int set = 0; set < SETS; ++set)
 #pragma unroll
-                    for (int u = 0; u < KN; ++u) {
-                        const uint4 qop = Qs[buffer][L::chunk(rb * 32 + c, 2 * u + h)];
-                        if constexpr (BF) {
-                            sc = mfma32(qop, kop[u], sc);
-                        } else {
-                            sc = mfma32(__uint_as_float(qop.x), __uint_as_float(kop[u].x), sc);
-                            sc = mfma32(__uint_as_float(qop.y), __uint_as_float(kop[u].y), sc);
-                            sc = mfma32(__uint_as_float(qop.z), __uint_as_float(kop[u].z), sc);
-                            sc = mfma32(__uint_as_float(qop.w), __uint_as_float(kop[u].w), sc);
-                        }
-                    }
-                    float s[16];
+                            for (int i = 0; i < 16; ++i) sc[set][i] = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = sc[i];
-                    if constexpr (CHANGED) {
-                        if (p.cap > 0.0f) cap_scores(s, p.scale, p.cap, p.cap_rcp);
-                    }
-                    const float unit = CHANGED && p.cap > 0.0f ? 1.0f : p.scale;
-                    float sum = 0.0f;
+                        for (int u = 0; u < KN; ++u) {
+                            // (chunk 2 u + h of row c, exchanged: the exchange of chunk h with 2 u's bits on top)
+                            const uint4 qop = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(Qs) + ((q_at ^ (u * 32)) + rb * 32 * L::CHUNKS * 16));
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int r = rb * 32 + 8 * u + 4 * h;
-                        const float4 top = *reinterpret_cast<const float4 *>(&row_max_s[buffer][r]), w = *reinterpret_cast<const float4 *>(&weight_s[buffer][r]);
-                        const float tops[4] = {top.x, top.y, top.z, top.w}, ws[4] = {w.x, w.y, w.z, w.w};
-                        int tokens[4];
-                        float slopes[4];
-                        if (CHANGED || masked) {
-                            const int4 t = *reinterpret_cast<const int4 *>(&token_s[buffer][r]);
-                            tokens[0] = t.x, tokens[1] = t.y, tokens[2] = t.z, tokens[3] = t.w;
-                        }
-                        if constexpr (CHANGED) {
-                            const float4 f = *reinterpret_cast<const float4 *>(&slope_s[buffer][r]);
-                            slopes[0] = f.x, slopes[1] = f.y, slopes[2] = f.z, slopes[3] = f.w;
-                        }
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            float v = s[4 * u + x];
-                            if constexpr (CHANGED) v = fmaf(-slopes[x], fabsf((float)(tokens[x] - entry)), v * unit) - tops[x];
-                            else v = fmaf(v, unit, -tops[x]);
-                            float e = __builtin_amdgcn_exp2f(v * kLog2e);
-                            float weight = ws[x];
-                            if (masked) {        // (both: what is not seen may hold anything)
-                                const int far = tokens[x] - entry;
-                                const bool seen = weight != 0.0f && (entry < prefix || (far >= 0 && (p.window <= 0 || far < p.window)));
-                                e = seen ? e : 0.0f;
-                                weight = seen ? weight : 0.0f;
+                            for (int set = 0; set < SETS; ++set) {
+                                const uint4 k = kop[set][u];
+                                if constexpr (BF) {
+                                    sc[set] = mfma32(qop, k, sc[set]);
+                                } else {
+                                    sc[set] = mfma32(__uint_as_float(qop.x), __uint_as_float(k.x), sc[set]);
+                                    sc[set] = mfma32(__uint_as_float(qop.y), __uint_as_float(k.y), sc[set]);
+                                    sc[set] = mfma32(__uint_as_float(qop.z), __uint_as_float(k.z), sc[set]);
+                                    sc[set] = mfma32(__uint_as_float(qop.w), __uint_as_float(k.w), sc[set]);
+                                }
                             }
-                            sum = fmaf(e, weight, sum);
                         }
+                        float s[SETS][16];
+#pragma unroll
+                        for (int set = 0; set < SETS; ++set) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[set][i] = sc[set][i];
+                            if constexpr (CAP) {
+                                if constexpr (BIAS) __builtin_amdgcn_sched_barrier(0);
+                                cap_parts(s[set], p.scale * p.cap_rcp);
+                                if constexpr (BIAS) __builtin_amdgcn_sched_barrier(0);
+                            }
+                        }
+                        const float unit = CAP ? p.cap : p.scale;
+                        float sum[SETS] = {};
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const int r = rb * 32 + 8 * u + 4 * h;
+                            const float4 top = *reinterpret_cast<const float4 *>(&row_max_s[buffer][r]), w = *reinterpret_cast<const float4 *>(&weight_s[buffer][r]);
+                            const float tops[4] = {top.x, top.y, top.z, top.w}, ws[4] = {w.x, w.y, w.z, w.w};
+                            int tokens[4] = {};
+                            float slopes[4] = {};
+                            if constexpr (BIAS || MASKED) {
+                                const int4 t = *reinterpret_cast<const int4 *>(&token_s[buffer][r]);
+                                tokens[0] = t.x, tokens[1] = t.y, tokens[2] = t.z, tokens[3] = t.w;
+                            }
+                            if constexpr (BIAS) {
+                                const float4 f = *reinterpret_cast<const float4 *>(&slope_s[buffer][r]);
+                                slopes[0] = f.x, slopes[1] = f.y, slopes[2] = f.z, slopes[3] = f.w;
+                            }
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                                for (int set = 0; set < SETS; ++set) {
+                                    const int entry = wave_entry + 32 * set + c;
+                                    float v = s[set][4 * u + x];
+                                    if constexpr (BIAS) v = fmaf(-slopes[x], fabsf((float)(tokens[x] - entry)), v * unit) - tops[x];
+                                    else v = fmaf(v, unit, -tops[x]);
+                                    float e = __builtin_amdgcn_exp2f(v * kLog2e), weight = ws[x];        // (0: top is infinite)
+                                    if constexpr (MASKED) {      // (both: what is not seen may hold anything)
+                                        // (no short circuits: they become branches)
+                                        const bool seen = ((uint32_t)(tokens[x] - entry) < reach) | (entry < prefix);
+                                        e = seen ? e : 0.0f;
+                                        weight = seen ? weight : 0.0f;
+                                    }
+                                    sum[set] = fmaf(e, weight, sum[set]);
+                                }
+                            if constexpr (BIAS || MASKED) __builtin_amdgcn_sched_barrier(0);     // (all rows' values at once cost registers)
+                        }
+#pragma unroll
+                        for (int set = 0; set < SETS; ++set) total[set] += sum[set];
                     }
-                    total += sum;
+                };
+                if constexpr (BIAS) {            // (one form: two cost registers)
+                    rows_of(std::true_type{});
+                } else {
+                    if (masked) rows_of(std::true_type{});
+                    else rows_of(std::false_type{});
                 }
             }
             if (row0 + ROWS < to) place(buffer ^ 1);
             __syncthreads();
         }
     }
-    total = halves_sum(total);
-    if (h == 0 && entry < n) {
-        const int part = split * p.Hkv + hk;
-        float *out = p.nsplit * p.Hkv == 1 ? p.mass : p.parts + (int64_t)part * p.tokens;
-        out[span.first + entry] = total;
+#pragma unroll
+    for (int set = 0; set < SETS; ++set) {
+        const float sum = halves_sum(total[set]);
+        const int entry = wave_entry + 32 * set + c;
+        if (h == 0 && entry < n) {
+            float *out = p.nsplit * p.Hkv == 1 ? p.mass : p.parts + (int64_t)(split * p.Hkv + hk) * p.tokens;
+            out[span.first + entry] = sum;
+        }
     }
 }
 
-constexpr int kJoinThreads = 128;
+// A wave takes the parts wave, wave + 8, ..; then the waves' sums.
+constexpr int kJoinWaves = 8, kJoinThreads = kJoinWaves * kWave;
 
 __global__ __launch_bounds__(kJoinThreads) void mass_join(PromptParams p) {
+    __shared__ float sums[kJoinWaves][kWave];
     int b;
     const int at_tile = fast_divide(p.by_tile, blockIdx.x, &b);
     const Span span = prompt_span(p, b);
-    const int entry = at_tile * kPromptTile + threadIdx.x;
-    if (entry >= span.n) return;
-    const float *from = p.parts + span.first + entry;
+    if (at_tile * kWave >= span.n) return;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, entry = at_tile * kWave + lane;
+    const float *from = p.parts + span.first + min(entry, span.n - 1);
     const int parts = p.nsplit * p.Hkv;
     float sum = 0.0f;
-    for (int i = 0; i < parts; i += 8) {
-        float v[8];
+    for (int i = wave; i < parts; i += 4 * kJoinWaves) {
+        float v[4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = i + u < parts ? from[(int64_t)(i + u) * p.tokens] : 0.0f;
+        for (int u = 0; u < 4; ++u) v[u] = i + u * kJoinWaves < parts ? from[(int64_t)(i + u * kJoinWaves) * p.tokens] : 0.0f;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) sum += v[u];
+        for (int u = 0; u < 4; ++u) sum += v[u];
     }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || entry >= span.n) return;
+#pragma unroll
+    for (int w = 1; w < kJoinWaves; ++w) sum += sums[w][lane];
     p.mass[span.first + entry] = sum;
 }
 
-// Runs that the rows of a block's entries are cut into: enough blocks for two on every CU, up to 16.
-int runs_of(int64_t blocks) {
-    int64_t runs = blocks > 0 ? 512 / blocks : 1;
+int64_t entry_tiles(int64_t entries, int per) { return (entries + per - 1) / per; }
+
+// Runs that the rows of a block's entries are cut into.  The first entries have many rows, the last few: some eight blocks a CU even that out.
+// At most 16, of 64 tokens at the least.
+int runs_of(int B, int Hkv, int max_len) {
+    const int64_t blocks = (int64_t)B * Hkv * entry_tiles(max_len, kMostEntries), most = ((int64_t)max_len + 63) / 64;
+    int64_t runs = blocks > 0 ? 2048 / blocks : 1;
+    if (runs > most) runs = most;
     return (int)(runs < 1 ? 1 : runs > 16 ? 16 : runs);
 }
 
@@ -207,7 +261,7 @@ using namespace pikv;
 extern "C" size_t pikv_prompt_mass_workspace_bytes(int32_t tokens, int32_t Hkv, int32_t B, int32_t max_len) {
     if (tokens < 0 || Hkv < 1 || Hkv > 256 || B < 0 || max_len < 0 || tokens > (1 << 23)) return 0;
     if (max_len > tokens) max_len = tokens;
-    return ((size_t)runs_of((int64_t)B * Hkv * prompt_tiles(max_len)) * Hkv * tokens * sizeof(float) + 255) / 256 * 256 + 256;
+    return ((size_t)runs_of(B, Hkv, max_len) * Hkv * tokens * sizeof(float) + 255) / 256 * 256 + 256;
 }
 
 extern "C" int pikv_prompt_mass(const void *q, const void *k, int32_t tokens, int64_t q_stride, int64_t k_stride, int32_t Hq,
@@ -218,8 +272,8 @@ extern "C" int pikv_prompt_mass(const void *q, const void *k, int32_t tokens, in
     const int rc = check_prompt(q, k, nullptr, false, tokens, q_stride, k_stride, 0, Hq, Hkv, D, dtype, B, max_len, scale, cap);
     if (rc != PIKV_OK) return rc;
     if (max_len > tokens) max_len = tokens;
-    const int64_t tiles = prompt_tiles(max_len), blocks = (int64_t)B * Hkv * tiles;
-    const int runs = runs_of(blocks);
+    const int64_t tiles = entry_tiles(max_len, kWaves * 32 * (dtype == PIKV_F32 ? sets_of<float> : sets_of<bf16>)), blocks = (int64_t)B * Hkv * tiles;
+    const int runs = runs_of(B, Hkv, max_len);
     if ((int64_t)B * Hkv * prompt_tiles((int64_t)max_len * (Hq / Hkv)) >= (1 << 23) || blocks * runs >= (1 << 23)) return PIKV_ERR_UNSUPPORTED;
     if (tokens == 0 || B == 0 || max_len == 0) return PIKV_OK;
     if (!q || !k || !cu_seqlens || !row_max || !row_norm || !mass) return PIKV_ERR_INVALID;
@@ -240,8 +294,13 @@ extern "C" int pikv_prompt_mass(const void *q, const void *k, int32_t tokens, in
     auto launch = [&](auto type, auto width) {
         typedef decltype(type) T;
         constexpr int W = decltype(width)::value;
-        if (cap > 0.0f || slopes) hipLaunchKernelGGL((mass_partial<T, W, true>), grid, threads, 0, st, p);
-        else hipLaunchKernelGGL((mass_partial<T, W, false>), grid, threads, 0, st, p);
+        if (cap > 0.0f) {
+            if (slopes) hipLaunchKernelGGL((mass_partial<T, W, true, true>), grid, threads, 0, st, p);
+            else hipLaunchKernelGGL((mass_partial<T, W, true, false>), grid, threads, 0, st, p);
+        } else {
+            if (slopes) hipLaunchKernelGGL((mass_partial<T, W, false, true>), grid, threads, 0, st, p);
+            else hipLaunchKernelGGL((mass_partial<T, W, false, false>), grid, threads, 0, st, p);
+        }
     };
     auto by_width = [&](auto type) {
         if (D == 32) launch(type, std::integral_constant<int, 32>{});
@@ -252,6 +311,6 @@ extern "C" int pikv_prompt_mass(const void *q, const void *k, int32_t tokens, in
     else by_width(bf16{});
     int done = launch_status();
     if (done != PIKV_OK || runs * Hkv == 1) return done;
-    hipLaunchKernelGGL(mass_join, dim3((unsigned)(B * tiles)), dim3(kJoinThreads), 0, st, p);
+    hipLaunchKernelGGL(mass_join, dim3((unsigned)(B * (((int64_t)max_len + kWave - 1) / kWave))), dim3(kJoinThreads), 0, st, p);
     return launch_status();
 }
