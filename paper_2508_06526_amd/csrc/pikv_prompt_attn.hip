@@ -138,6 +138,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
 #pragma unroll
         for (int s = 0; s < QN; ++s) q[s] = load16(from + (2 * s + h) * 16);
     }
+#pragma unroll
+    for (int s = 0; s < QN; ++s) hold_operand(q[s]);         // complete here, not behind requests in the loop
     f32x16_t acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)

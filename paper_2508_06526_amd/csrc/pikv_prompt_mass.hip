@@ -100,6 +100,10 @@ __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
         }
     };
     float total[SETS] = {};
+#pragma unroll
+    for (int set = 0; set < SETS; ++set)
+#pragma unroll
+        for (int s = 0; s < KN; ++s) hold_operand(kop[set][s]);      // complete here, not behind requests in the loop
     if (from < to) {                             // (uniform)
         request(from);
         place(0);
