@@ -16,21 +16,25 @@
 namespace pikv {
 namespace {
 
-constexpr int kWaves = 4, kThreads = kWaves * kWave, kWaveRows = 32;      // rows of a wave
+constexpr int kWaveRows = 32;            // rows of a wave
+// bf16 rows of 64 values and more: 8 waves, as a tile's way into LDS takes a sixth of the time of 4.  (fp32: matrix instructions of four times the
+// length; rows of 32 values: a tile is 256 pieces.)
+template <typename T, int D>
+constexpr int threads_of = sizeof(T) == 2 && D >= 64 ? 512 : 256;
 
 // LDS tiles of KEYS entries x D values, in 16-byte chunks, a row's chunks exchanged by an xor so that the reads of a wave spread over
 // the banks: K is read as one chunk of 32 entries each, V (bf16) as 64 bytes of 4 neighbouring entries each.
-template <typename T, int D, int THREADS = kThreads>
+template <typename T, int D, bool SPLIT>
 struct Tile {
-    static constexpr int KEYS = sizeof(T) == 2 ? 64 : 32;
+    static constexpr int KEYS = sizeof(T) == 2 && !SPLIT ? 64 : 32;
+    static constexpr int THREADS = SPLIT ? kWave : threads_of<T, D>;  // that bring a tile
     static constexpr int CHUNKS = D * (int)sizeof(T) / 16;            // of a row
-    static constexpr int PER_THREAD = KEYS * CHUNKS / THREADS;       // of a tile
+    static constexpr int PER_THREAD = KEYS * CHUNKS / THREADS;        // of a tile
     static constexpr int PER_LINE = CHUNKS >= 16 ? 1 : 16 / CHUNKS;   // rows of 256 bytes
-    static __device__ __forceinline__ int k_chunk(int key, int c) { return key * CHUNKS + (c ^ ((key / PER_LINE) & (CHUNKS < 16 ? CHUNKS - 1 : 15))); }
-    static __device__ __forceinline__ int v_chunk(int key, int c) {
-        if constexpr (sizeof(T) == 2) return key * CHUNKS + (c ^ (((key / PER_LINE) & (CHUNKS / 4 - 1)) << 2));
-        else return key * CHUNKS + c;
-    }
+    static constexpr __device__ __forceinline__ int k_exchange(int key) { return (key / PER_LINE) & (CHUNKS < 16 ? CHUNKS - 1 : 15); }
+    static constexpr __device__ __forceinline__ int v_exchange(int key) { return sizeof(T) == 2 ? ((key / PER_LINE) & (CHUNKS / 4 - 1)) << 2 : 0; }
+    static __device__ __forceinline__ int k_chunk(int key, int c) { return key * CHUNKS + (c ^ k_exchange(key)); }
+    static __device__ __forceinline__ int v_chunk(int key, int c) { return key * CHUNKS + (c ^ v_exchange(key)); }
 };
 
 typedef short s16x4_lds __attribute__((ext_vector_type(4)));
@@ -39,47 +43,17 @@ __device__ __forceinline__ uint2 read_transposed(const void *at) {
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)at));
 }
 
-// What a wave holds at the end goes to its rows: O^T / l, and the statistics.
-template <typename T, int D>
-__device__ __forceinline__ void write_rows(const PromptParams &p, Span span, int hk, int wave_row, int rows, const f32x16_t (&acc)[D / 32], float top, float shift,
-                                           float l) {
-    l = halves_sum(l);
-    top = halves_max(top);
-    // (rows found again: not carried through the loop)
-    const int my_lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), my_h = my_lane >> 5;
-    const int my_row = wave_row + (my_lane & 31), my_token = row_token(p, my_row);
-    if (my_row >= rows) return;
-    const int64_t to = (int64_t)(span.first + my_token) * p.Hq + hk * p.G + my_row - my_token * p.G;
-    if (p.row_max && my_h == 0) {
-        p.row_max[to] = top * p.unit;
-        p.row_norm[to] = l * __builtin_amdgcn_exp2f((shift - (top == -INFINITY ? 0.0f : top)) * p.unit_log2);
-    }
-    const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;    // (a NaN stays one)
-    T *out = static_cast<T *>(p.out) + to * D;
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            float v[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] = acc[d][4 * u + x] * inv;
-            T *at = out + d * 32 + 8 * u + 4 * my_h;
-            if constexpr (sizeof(T) == 2) {
-                uint2 packed[1];
-                split_bf16(v, packed);
-                *reinterpret_cast<uint2 *>(at) = packed[0];
-            } else {
-                *reinterpret_cast<float4 *>(at) = make_float4(v[0], v[1], v[2], v[3]);
-            }
-        }
-}
-
-// CAP: scores capped by a tanh; BIAS: with a distance term.
-template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
-    typedef Tile<T, D> L;
+// CAP: scores capped by a tanh; BIAS: with a distance term.  SPLIT: for few rows, a block takes 32 of them and its waves every fourth tile each, by
+// themselves; their results are joined at the end.
+constexpr int kSplitWaves = 4;
+template <typename T, int D, bool SPLIT>
+constexpr int block_waves = SPLIT ? kSplitWaves : threads_of<T, D> / kWave;
+template <typename T, int D, bool CAP, bool BIAS, bool SPLIT>
+__global__ __launch_bounds__((block_waves<T, D, SPLIT> * kWave), (SPLIT && D == 128 ? 1 : 2)) void prompt_attn(PromptParams p) {
+    typedef Tile<T, D, SPLIT> L;
+    constexpr int WAVES = block_waves<T, D, SPLIT>, ROWS = SPLIT ? kWaveRows : WAVES * kWaveRows, THREADS = L::THREADS;
     constexpr bool BF = sizeof(T) == 2;
-    constexpr int KEYS = L::KEYS, KB = KEYS / 32, DT = D / 32, BUFFERS = 2;
+    constexpr int KEYS = L::KEYS, KB = KEYS / 32, DT = D / 32, BUFFERS = SPLIT ? WAVES : 2, STEP = SPLIT ? WAVES : 1;
     constexpr int QN = D * (int)sizeof(T) / 32;                       // 16-byte pieces of a lane's query
     __shared__ __attribute__((aligned(16))) uint4 Ks[BUFFERS][KEYS * L::CHUNKS], Vs[BUFFERS][KEYS * L::CHUNKS];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -90,18 +64,18 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
     int at_tile = fast_divide(p.by_tile, rest, &b);                   // (by_tile: sequences)
     at_tile = p.tiles - 1 - at_tile;
     const Span span = prompt_span(p, b);
-    const int n = span.n, rows = n * p.G, row0 = at_tile * kPromptTile;
+    const int n = span.n, rows = n * p.G, row0 = at_tile * ROWS;
     if (row0 >= rows) return;
     const int prefix = p.prefix ? __builtin_amdgcn_readfirstlane(min(max(p.prefix[b], 0), n)) : 0;
-    const int last_token = row_token(p, min(row0 + kPromptTile, rows) - 1), first_token = row_token(p, row0);
+    const int last_token = row_token(p, min(row0 + ROWS, rows) - 1), first_token = row_token(p, row0);
     // tiles 0 .. prefix_tiles - 1, then window_tile .. last_tile
     const int prefix_tiles = (prefix + KEYS - 1) / KEYS;
     const int window_tile = max(prefix_tiles, p.window > 0 ? max(first_token - p.window + 1, 0) / KEYS : 0);
-    const int last_tile = max(prefix_tiles - 1, last_token / KEYS);
-    auto after = [&](int t) { return t + 1 < prefix_tiles ? t + 1 : max(t + 1, window_tile); };
+    const int last_tile = max(prefix_tiles - 1, last_token / KEYS), count = prefix_tiles + max(last_tile - window_tile + 1, 0);
+    auto tile_at = [&](int i) { return i < prefix_tiles ? i : i - prefix_tiles + window_tile; };
 
     // the wave's rows
-    const int wave_row = row0 + wave * kWaveRows;
+    const int wave_row = row0 + (SPLIT ? 0 : wave) * kWaveRows;
     const int row = min(wave_row + c, rows - 1), token = row_token(p, row), head = hk * p.G + row - token * p.G;
     const int wave_first = row_token(p, min(wave_row, rows - 1)), wave_last = row_token(p, min(wave_row + kWaveRows, rows) - 1);
     // Scores are kept as they come: products (capped: parts of the cap) that p.unit makes scores of, or with a distance term scores.
@@ -119,9 +93,10 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
     auto request = [&](uint32_t (&to)[L::PER_THREAD][4], const char *base, int64_t stride, int t) {
         const int here = min(n - t * KEYS, KEYS);
         const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + t * KEYS * stride), 0, (uint32_t)(here - 1) * (uint32_t)stride + D * (int)sizeof(T), 0x00020000);
-        const uint32_t at = opaque((tid / L::CHUNKS) * (uint32_t)stride + (tid % L::CHUNKS) * 16);
+        const int tid = (int)opaque(threadIdx.x) & (THREADS - 1);
+        const uint32_t at = (tid / L::CHUNKS) * (uint32_t)stride + (tid % L::CHUNKS) * 16;
 #pragma unroll
-        for (int u = 0; u < L::PER_THREAD; ++u) buffer_load<16, false>(to[u], from, at + u * (kThreads / L::CHUNKS) * (uint32_t)stride);
+        for (int u = 0; u < L::PER_THREAD; ++u) buffer_load<16, false>(to[u], from, at + u * (THREADS / L::CHUNKS) * (uint32_t)stride);
     };
     // Whether rows first .. last of tokens see all entries of a tile.
     auto seen_whole = [&](int t, int first, int last) {
@@ -139,18 +114,20 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) bad |= special(vr[u][i]) || (BF && special(vr[u][i] << 16));
         }
-        // pieces tid, tid + kThreads, ..: whole lines further on (fp32 rows of 128 values: half the exchange's 16 rows)
-        constexpr int LINES = kThreads / L::CHUNKS;
-        const uint32_t to_k = opaque(L::k_chunk(tid / L::CHUNKS, tid % L::CHUNKS) * 16 + buffer * (int)sizeof(Ks[0]));
-        const uint32_t to_v = opaque(L::v_chunk(tid / L::CHUNKS, tid % L::CHUNKS) * 16 + buffer * (int)sizeof(Vs[0]));
+        // pieces tid, tid + THREADS, ..: the exchange of rows tid / CHUNKS + u LINES is that of either
+        constexpr int LINES = THREADS / L::CHUNKS;
+        const int tid = (int)opaque(threadIdx.x) & (THREADS - 1);
+        const uint32_t to_k = L::k_chunk(tid / L::CHUNKS, tid % L::CHUNKS) * 16 + buffer * (int)sizeof(Ks[0]);
+        const uint32_t to_v = L::v_chunk(tid / L::CHUNKS, tid % L::CHUNKS) * 16 + buffer * (int)sizeof(Vs[0]);
         auto write_v = [&](auto of) {
 #pragma unroll
             for (int u = 0; u < L::PER_THREAD; ++u)
-                *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(Vs) + to_v + u * kThreads * 16) = make_uint4(of(vr[u][0]), of(vr[u][1]), of(vr[u][2]), of(vr[u][3]));
+                *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(Vs) + ((to_v ^ (L::v_exchange(u * LINES) * 16)) + u * THREADS * 16)) =
+                    make_uint4(of(vr[u][0]), of(vr[u][1]), of(vr[u][2]), of(vr[u][3]));
         };
 #pragma unroll
         for (int u = 0; u < L::PER_THREAD; ++u)
-            *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(Ks) + ((LINES == 8 ? to_k ^ (u % 2 * 128) : to_k) + u * kThreads * 16)) =
+            *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(Ks) + ((to_k ^ (L::k_exchange(u * LINES) * 16)) + u * THREADS * 16)) =
                 make_uint4(kr[u][0], kr[u][1], kr[u][2], kr[u][3]);
         if (__any(bad))
             write_v([&](uint32_t w) { return (special(w) ? 0u : w & (BF ? 0xffff0000u : 0xffffffffu)) | (BF && !special(w << 16) ? w & 0xffffu : 0u); });
@@ -159,13 +136,20 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
         return bad;
     };
     auto placed = [&](int t, bool bad) {         // the barrier behind it: whether the tile held any
-        if (!seen_whole(t, first_token, last_token)) return __syncthreads_or(bad) != 0;
-        __syncthreads();
-        return false;
+        if constexpr (SPLIT) {
+            wave_lds_order();
+            return __any(bad) != 0;
+        } else {
+            if (!seen_whole(t, first_token, last_token)) return __syncthreads_or(bad) != 0;
+            __syncthreads();
+            return false;
+        }
     };
-    int tile = prefix_tiles > 0 ? 0 : window_tile;
-    request(kr, Kb, k_bytes, tile);
-    request(vr, Vb, v_bytes, tile);
+    int at = SPLIT ? wave : 0, buffer = SPLIT ? wave : 0;
+    if (!SPLIT || at < count) {
+        request(kr, Kb, k_bytes, tile_at(at));
+        request(vr, Vb, v_bytes, tile_at(at));
+    }
     // the query operand: 16-byte pieces 2 s + h of row c
     uint4 q[QN];
     {
@@ -186,12 +170,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
     // accumulators that get an infinity at the end (a NaN: both), 32 to a word
     constexpr int WORDS = (DT * 16 + 31) / 32;
     uint32_t most_inf[WORDS] = {}, least_inf[WORDS] = {};
-    bool odd = placed(tile, place(tile, 0));
-    int buffer = 0;
-    for (; tile <= last_tile; buffer ^= 1) {
-        const int next = after(tile), key0 = tile * KEYS;
+    bool odd = (!SPLIT || at < count) && placed(tile_at(at), place(tile_at(at), buffer));
+    for (; at < count; at += STEP) {
+        const int tile = tile_at(at), next = tile_at(at + STEP), key0 = tile * KEYS;
+        const bool more = at + STEP < count;
         const int lane = (int)opaque(tid) & (kWave - 1), c = lane & 31, h = lane >> 5;      // (derived again in every round: registers)
-        if (next <= last_tile) request(kr, Kb, k_bytes, next);
+        if (more) request(kr, Kb, k_bytes, next);
         const bool in_prefix = key0 < prefix;
         const bool any = in_prefix || (key0 <= wave_last && (p.window <= 0 || wave_first - (key0 + KEYS - 1) < p.window));
         if (any) {
@@ -224,7 +208,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
                     for (int i = 0; i < 16; ++i) s[kb][i] = fmaf(-slope, fabsf((float)(first + 8 * (i >> 2) + (i & 3))), s[kb][i] * (CAP ? p.cap : p.scale));
                 }
             }
-            if (next <= last_tile) request(vr, Vb, v_bytes, next);      // (behind the first product: its registers)
+            if (more) request(vr, Vb, v_bytes, next);       // (behind the first product: its registers)
             const bool masked = !seen_whole(tile, wave_first, wave_last);
             // the lane's row sees entries low .. token and those below the prefix
             const int low = p.window > 0 ? max(token - p.window + 1, 0) : 0;
@@ -302,9 +286,10 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
                 }
             }
         }
-        if (!any && next <= last_tile) request(vr, Vb, v_bytes, next);
-        odd = next <= last_tile && placed(next, place(next, buffer ^ 1));
-        tile = next;
+        if (!any && more) request(vr, Vb, v_bytes, next);
+        if constexpr (SPLIT) wave_lds_order();       // (the tile's reads before the next one's writes)
+        else buffer ^= 1;
+        odd = more && placed(next, place(next, buffer));
     }
     bool any_inf = false;
 #pragma unroll
@@ -316,305 +301,88 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn(PromptParams p) {
             if (least_inf[j / 32] >> (j & 31) & 1u) acc[j >> 4][j & 15] -= INFINITY;
         }
     }
-    write_rows<T, D>(p, span, hk, wave_row, rows, acc, top, shift, l);
+    l = halves_sum(l);
+    top = halves_max(top);
+    // (found again: not carried through the loop)
+    const int my_lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), my_c = my_lane & 31, my_h = my_lane >> 5;
+    const int my_row = wave_row + my_c, my_token = row_token(p, my_row);
+    const int64_t to = (int64_t)(span.first + my_token) * p.Hq + hk * p.G + my_row - my_token * p.G;
+    auto write_stats = [&] {
+        if (p.row_max && my_h == 0) {
+            p.row_max[to] = top * p.unit;
+            p.row_norm[to] = l * __builtin_amdgcn_exp2f((shift - (top == -INFINITY ? 0.0f : top)) * to_log2);
+        }
+    };
+    auto inverse = [&] { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; };       // (a NaN stays one)
+    auto write4 = [&](int j, const float (&v)[4]) {          // accumulators j .. j + 3
+        T *at = static_cast<T *>(p.out) + to * D + (j >> 4) * 32 + 8 * (j >> 2 & 3) + 4 * my_h;
+        if constexpr (BF) {
+            uint2 packed[1];
+            split_bf16(v, packed);
+            *reinterpret_cast<uint2 *>(at) = packed[0];
+        } else {
+            *reinterpret_cast<float4 *>(at) = make_float4(v[0], v[1], v[2], v[3]);
+        }
+    };
+    if constexpr (SPLIT) {
+        // the waves' accumulators over their tiles in LDS; each wave joins a quarter of them
+        constexpr int N = DT * 16, MINE = N / WAVES;
+        static_assert(WAVES * N * kWave * 4 <= (int)(sizeof(Ks) + sizeof(Vs)) && N % WAVES == 0, "joined where the tiles were");
+        __shared__ float base_s[WAVES][kWaveRows], l_s[WAVES][kWaveRows], top_s[WAVES][kWaveRows];
+        __syncthreads();
+        float *mine = reinterpret_cast<float *>(wave < WAVES / 2 ? &Ks[0][0] : &Vs[0][0]) + (wave % (WAVES / 2)) * N * kWave;
+#pragma unroll
+        for (int j = 0; j < N; ++j) mine[j * kWave + my_lane] = acc[j >> 4][j & 15];
+        if (my_h == 0) {
+            base_s[wave][my_c] = base;
+            l_s[wave][my_c] = l;
+            top_s[wave][my_c] = top;
+        }
+        __syncthreads();
+        base = top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            base = fmaxf(base, base_s[w][my_c]);
+            top = fmaxf(top, top_s[w][my_c]);
+        }
+        shift = base == -INFINITY ? 0.0f : base;
+        l = 0.0f;
+        float v[MINE] = {};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float factor = __builtin_amdgcn_exp2f((base_s[w][my_c] - shift) * to_log2);
+            l = fmaf(l_s[w][my_c], factor, l);
+            const float *from = reinterpret_cast<const float *>(w < WAVES / 2 ? &Ks[0][0] : &Vs[0][0]) + ((w % (WAVES / 2)) * N + wave * MINE) * kWave;
+#pragma unroll
+            for (int j = 0; j < MINE; ++j) v[j] = fmaf(from[j * kWave + my_lane], factor, v[j]);
+        }
+        if (my_row >= rows) return;
+        if (wave == 0) write_stats();
+        const float inv = inverse();
+#pragma unroll
+        for (int j = 0; j < MINE; j += 4) {
+            const float four[4] = {v[j] * inv, v[j + 1] * inv, v[j + 2] * inv, v[j + 3] * inv};
+            write4(wave * MINE + j, four);
+        }
+    } else {
+        if (my_row >= rows) return;
+        write_stats();
+        const float inv = inverse();
+#pragma unroll
+        for (int j = 0; j < DT * 16; j += 4) {
+            const float four[4] = {acc[j >> 4][j & 15] * inv, acc[j >> 4][(j & 15) + 1] * inv, acc[j >> 4][(j & 15) + 2] * inv, acc[j >> 4][(j & 15) + 3] * inv};
+            write4(j, four);
+        }
+    }
 }
-// (a tile of rows of 32 values is 256 pieces)
-template <int D>
-constexpr int staged_threads = D == 32 ? 256 : 512;
 
-// The bf16 form.  Matrix instructions and the softmax's take about as long, and a SIMD has registers for two waves, so a wave overlaps
-// them itself, 32 entries at a time: a stage forms the scores of the next 32 (K), the weights of these, and the outputs of the last
-// (V), none of which waits for another.  A tile of 64 entries is two stages and one barrier:
-//     stage 1:  scores of the tile's second half,  weights of its first,   outputs of the tile before's second
-//     stage 2:  scores of the next tile's first,   weights of its second,  outputs of its first
-template <int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(staged_threads<D>, 2) void prompt_attn_staged(PromptParams p) {
-    constexpr int THREADS = staged_threads<D>, ROWS = THREADS / 2;      // (32 rows of 64 lanes)
-    typedef Tile<bf16, D, THREADS> L;
-    constexpr int KEYS = L::KEYS, DT = D / 32, QN = D / 16, WORDS = (DT * 16 + 31) / 32;
-    __shared__ __attribute__((aligned(16))) uint4 Ks[2][KEYS * L::CHUNKS], Vs[2][KEYS * L::CHUNKS];
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // the blocks with the most entries first
-    int hk, b;
-    const int rest = fast_divide(p.by_head, blockIdx.x, &hk);
-    int at_tile = fast_divide(p.by_tile, rest, &b);                   // (by_tile: sequences)
-    at_tile = p.tiles - 1 - at_tile;
-    const Span span = prompt_span(p, b);
-    const int n = span.n, rows = n * p.G, row0 = at_tile * ROWS;
-    if (row0 >= rows) return;
-    const int prefix = p.prefix ? __builtin_amdgcn_readfirstlane(min(max(p.prefix[b], 0), n)) : 0;
-    const int last_token = row_token(p, min(row0 + ROWS, rows) - 1), first_token = row_token(p, row0);
-    // tiles 0 .. prefix_tiles - 1, then window_tile .. last_tile
-    const int prefix_tiles = (prefix + KEYS - 1) / KEYS;
-    const int window_tile = max(prefix_tiles, p.window > 0 ? max(first_token - p.window + 1, 0) / KEYS : 0);
-    const int last_tile = max(prefix_tiles - 1, last_token / KEYS);
-    auto after = [&](int t) { return t + 1 < prefix_tiles ? t + 1 : max(t + 1, window_tile); };
-
-    auto opaque = [](uint32_t v) {           // (else an address per read is carried through the loop)
-        asm volatile("" : "+v"(v));
-        return v;
-    };
-    // the wave's rows
-    const int wave_row = row0 + wave * kWaveRows;
-    const int wave_first = row_token(p, min(wave_row, rows - 1)), wave_last = row_token(p, min(wave_row + kWaveRows, rows) - 1);
-    int token;
-    float slope = 0.0f;
-
-    const int64_t k_bytes = p.k_stride * 2, v_bytes = p.v_stride * 2;
-    const char *Kb = static_cast<const char *>(p.k) + span.first * k_bytes + hk * D * 2;
-    const char *Vb = static_cast<const char *>(p.v) + span.first * v_bytes + hk * D * 2;
-    uint32_t kr[L::PER_THREAD][4], vr[L::PER_THREAD][4];
-    // A tile's rows; those past the end read as zeros.
-    auto request = [&](uint32_t (&to)[L::PER_THREAD][4], const char *base, int64_t stride, int t) {
-        const int here = min(n - t * KEYS, KEYS);
-        const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + t * KEYS * stride), 0, (uint32_t)(here - 1) * (uint32_t)stride + D * 2, 0x00020000);
-        const int tid = (int)opaque(threadIdx.x);
-        const uint32_t at = (tid / L::CHUNKS) * (uint32_t)stride + (tid % L::CHUNKS) * 16;
-#pragma unroll
-        for (int u = 0; u < L::PER_THREAD; ++u) buffer_load<16, false>(to[u], from, at + u * (THREADS / L::CHUNKS) * (uint32_t)stride);
-    };
-    auto place_k = [&](int buffer) {
-        const int tid = (int)opaque(threadIdx.x);
-        const uint32_t at = L::k_chunk(tid / L::CHUNKS, tid % L::CHUNKS) * 16 + buffer * (int)sizeof(Ks[0]);
-#pragma unroll
-        for (int u = 0; u < L::PER_THREAD; ++u)
-            *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(Ks) + at + u * THREADS * 16) = make_uint4(kr[u][0], kr[u][1], kr[u][2], kr[u][3]);
-    };
-    // Whether rows first .. last of tokens see all of `entries` from key0 on.
-    auto seen_whole = [&](int key0, int entries, int first, int last) {
-        return key0 + entries <= n && (key0 + entries <= prefix || (key0 + entries - 1 <= first && (p.window <= 0 || last - key0 < p.window)));
-    };
-    // A value that is no number stays out of the rows that do not see its entry: 0 x NaN is NaN.  Where a tile is not seen whole such
-    // values go to LDS as zeros, and the block is told (rare).
-    auto place_v = [&](int t, int buffer) {
-        auto special = [](uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; };
-        bool bad = false;
-        if (!seen_whole(t * KEYS, KEYS, first_token, last_token)) {
-#pragma unroll
-            for (int u = 0; u < L::PER_THREAD; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) bad |= special(vr[u][i]) || special(vr[u][i] << 16);
-        }
-        const int tid = (int)opaque(threadIdx.x);
-        const uint32_t at = L::v_chunk(tid / L::CHUNKS, tid % L::CHUNKS) * 16 + buffer * (int)sizeof(Vs[0]);
-        auto write = [&](auto of) {
-#pragma unroll
-            for (int u = 0; u < L::PER_THREAD; ++u)
-                *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(Vs) + at + u * THREADS * 16) = make_uint4(of(vr[u][0]), of(vr[u][1]), of(vr[u][2]), of(vr[u][3]));
-        };
-        if (__any(bad)) write([&](uint32_t w) { return (special(w) ? 0u : w & 0xffff0000u) | (special(w << 16) ? 0u : w & 0xffffu); });
-        else write([](uint32_t w) { return w; });
-        return bad;
-    };
-
-    int tile = prefix_tiles > 0 ? 0 : window_tile, next = after(tile);
-    request(kr, Kb, k_bytes, tile);
-    request(vr, Vb, v_bytes, tile);
-    // the query operand: 16-byte pieces 2 s + h of row c
-    uint4 q[QN];
-    {
-        const int lane = tid & (kWave - 1), row = min(wave_row + (lane & 31), rows - 1);
-        token = row_token(p, row);
-        const int head = hk * p.G + row - token * p.G;
-        if constexpr (BIAS) slope = p.slopes[head];
-        const char *from = static_cast<const char *>(p.q) + ((int64_t)(span.first + token) * p.q_stride + (int64_t)head * D) * 2;
-#pragma unroll
-        for (int s = 0; s < QN; ++s) q[s] = load16(from + (2 * s + (lane >> 5)) * 16);
-    }
-    place_k(0);
-    if (next <= last_tile) request(kr, Kb, k_bytes, next);
-#pragma unroll
-    for (int s = 0; s < QN; ++s) hold_operand(q[s]);         // complete here, not behind requests in the loop
-#pragma unroll
-    for (int u = 0; u < L::PER_THREAD; ++u) Vs[1][tid + u * THREADS] = make_uint4(0u, 0u, 0u, 0u);      // (what the first stage's outputs are of)
-    __syncthreads();
-
-    f32x16_t acc[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
-    // The maximum of the lane's scores so far; what they are taken relative to, which follows it only when a weight would pass 2^8:
-    // most stages then leave the accumulators alone.
-    float top = -INFINITY, base = -INFINITY, shift = 0.0f, l = 0.0f;        // shift: base, 0 while nothing has been seen
-    // accumulators that get an infinity at the end (a NaN: both), 32 to a word
-    uint32_t most_inf[WORDS] = {}, least_inf[WORDS] = {};
-
-    auto scores_of = [&](int buffer, int half) {             // of entries half * 32 .. of a tile
-        const int lane = (int)opaque(threadIdx.x) & (kWave - 1), c = lane & 31, h = lane >> 5;
-        // chunk 2 u + h of entry c, exchanged: the exchange of chunk h with 2 u's bits on top
-        const uint32_t at = opaque(L::k_chunk(c, h) * 16 + buffer * (int)sizeof(Ks[0]));
-        f32x16_t sc;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
-#pragma unroll
-        for (int u = 0; u < QN; ++u)
-            sc = mfma32(*reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(Ks) + ((at ^ (u * 32)) + half * 32 * L::CHUNKS * 16)), q[u], sc);
-        return sc;
-    };
-    auto outputs_of = [&](const uint4 (&weights)[2], int buffer, int half) {
-        // 16 lanes read 4 entries x 16 values: lane g of them entry g / 4, values 4 (g % 4) .. of the 16 (lane & 16 ..)
-        const int lane = (int)opaque(threadIdx.x) & (kWave - 1), h = lane >> 5, g = lane & 15, value = (lane & 16) + 4 * (g & 3);
-        const uint32_t at = opaque(L::v_chunk(4 * h + (g >> 2), value >> 3) * 16 + (value & 7) * 2 + buffer * (int)sizeof(Vs[0]));
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const char *from = reinterpret_cast<const char *>(Vs) + ((at ^ (d * 64)) + (half * 32 + 16 * st) * L::CHUNKS * 16);
-                const uint2 lo = read_transposed(from), hi = read_transposed(from + 8 * L::CHUNKS * 16);
-                acc[d] = mfma32(make_uint4(lo.x, lo.y, hi.x, hi.y), weights[st], acc[d]);
-            }
-    };
-    auto seen = [&](int key) {               // the lane's row sees entries low .. token and those below the prefix
-        const int low = p.window > 0 ? max(token - p.window + 1, 0) : 0;
-        return ((uint32_t)(key - low) <= (uint32_t)(token - low)) | (key < prefix);
-    };
-    f32x16_t sc;
-    bool rescale = false;
-    float corr = 1.0f;
-    uint4 weights[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
-    // Scores sc are those of the 32 entries from key0 on.
-    auto stage = [&](int key0, int k_buffer, int k_half, int v_buffer, int v_half) {
-        float s[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = sc[i];
-        const int h = ((int)opaque(threadIdx.x) >> 5) & 1;
-        if constexpr (CAP) cap_parts(s, p.scale * p.cap_rcp);
-        if constexpr (BIAS) {
-            const int first = key0 + 4 * h - token;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = fmaf(-slope, fabsf((float)(first + 8 * (i >> 2) + (i & 3))), s[i] * (CAP ? p.cap : p.scale));
-        }
-        if (!seen_whole(key0, 32, wave_first, wave_last)) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (!seen(key0 + 8 * (i >> 2) + 4 * h + (i & 3))) s[i] = -INFINITY;
-        }
-        if (rescale) {                       // (uniform) what the last stage's maxima asked for, behind the outputs it added
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[d][i] *= corr;
-        }
-        float most = s[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
-        top = fmaxf(top, most);
-        rescale = __any(most > base + p.margin);
-        if (rescale) {
-            const float now = halves_max(fmaxf(top, base)), next_shift = now == -INFINITY ? 0.0f : now;
-            corr = __builtin_amdgcn_exp2f((base - next_shift) * p.unit_log2);
-            l *= corr;
-            base = now;
-            shift = next_shift;
-        }
-        // The products in turn, a piece of the softmax in the shadow of each, operands read from LDS a few products ahead.  (In this order:
-        // left to itself the compiler puts the products together.)
-        const int lane = (int)opaque(threadIdx.x) & (kWave - 1), c = lane & 31, g = lane & 15, value = (lane & 16) + 4 * (g & 3);
-        const uint32_t k_at = L::k_chunk(c, h) * 16 + k_buffer * (int)sizeof(Ks[0]) + k_half * 32 * L::CHUNKS * 16;
-        const uint32_t v_at = L::v_chunk(4 * h + (g >> 2), value >> 3) * 16 + (value & 7) * 2 + v_buffer * (int)sizeof(Vs[0]) + v_half * 32 * L::CHUNKS * 16;
-        constexpr int PRODUCTS = QN + 2 * DT, PER = 16 / PRODUCTS, AHEAD = 4;
-        static_assert(QN == 2 * DT && PER * PRODUCTS == 16, "as many products of either kind; all weights among them");
-        uint4 operand[PRODUCTS];
-        auto read = [&](int i) {
-            if (i % 2 == 0) {
-                operand[i] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(Ks) + (k_at ^ (i / 2 * 32)));
-            } else {
-                const char *from = reinterpret_cast<const char *>(Vs) + ((v_at ^ (i / 2 % DT * 64)) + i / 2 / DT * 16 * L::CHUNKS * 16);
-                const uint2 lo = read_transposed(from), hi = read_transposed(from + 8 * L::CHUNKS * 16);
-                operand[i] = make_uint4(lo.x, lo.y, hi.x, hi.y);
-            }
-        };
-        float sum = 0.0f;
-        const float shift_log2 = -shift * p.unit_log2;
-        f32x16_t next_sc;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) next_sc[i] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < (AHEAD < PRODUCTS ? AHEAD : PRODUCTS); ++i) read(i);
-        uint4 formed[2];
-#pragma unroll
-        for (int i = 0; i < PRODUCTS; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
-            if (i + AHEAD < PRODUCTS) read(i + AHEAD);
-            if (i % 2 == 0) next_sc = mfma32(operand[i], q[i / 2], next_sc);
-            else acc[i / 2 % DT] = mfma32(operand[i], weights[i / 2 / DT], acc[i / 2 % DT]);
-#pragma unroll
-            for (int x = i * PER; x < (i + 1) * PER; ++x) {
-                s[x] = __builtin_amdgcn_exp2f(fmaf(s[x], p.unit_log2, shift_log2));
-                sum += s[x];
-                asm volatile("" : "+v"(s[x]), "+v"(sum));
-            }
-            uint4 packed[1];
-            if ((i + 1) * PER == 8) {
-                split_bf16(s, packed);
-                formed[0] = packed[0];
-            } else if ((i + 1) * PER == 16) {
-                split_bf16(s + 8, packed);
-                formed[1] = packed[0];
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        weights[0] = formed[0];
-        weights[1] = formed[1];
-        hold_operand(weights[0]);            // (formed here, beside the products: not where they are used)
-        hold_operand(weights[1]);
-        sc = next_sc;
-        l += sum;
-        asm volatile("" : "+v"(l));
-    };
-    sc = scores_of(0, 0);
-    int buffer = 0;
-    for (;; buffer ^= 1) {
-        const bool more = next <= last_tile;
-        stage(tile * KEYS, buffer, 1, buffer ^ 1, 1);
-        if (more) place_k(buffer ^ 1);
-        const bool bad = place_v(tile, buffer);
-        bool odd = false;
-        if (!seen_whole(tile * KEYS, KEYS, first_token, last_token)) odd = __syncthreads_or(bad) != 0;
-        else __syncthreads();
-        const int next_but_one = after(next);
-        if (more) {
-            request(vr, Vb, v_bytes, next);
-            if (next_but_one <= last_tile) request(kr, Kb, k_bytes, next_but_one);
-        }
-        stage(tile * KEYS + 32, buffer ^ 1, 0, buffer, 0);
-        if (odd) {
-            const int h = ((int)opaque(threadIdx.x) >> 5) & 1;
-            for (int key = tile * KEYS; key < min(tile * KEYS + KEYS, n); ++key) {
-                if (!seen(key)) continue;
-                const bf16 *row = reinterpret_cast<const bf16 *>(Vb + key * v_bytes);
-#pragma unroll
-                for (int j = 0; j < DT * 16; ++j) {
-                    const float v = load_scalar<bf16>(row, (j >> 4) * 32 + 8 * (j >> 2 & 3) + 4 * h + (j & 3));
-                    most_inf[j / 32] |= v == INFINITY || v != v ? 1u << (j & 31) : 0u;
-                    least_inf[j / 32] |= v == -INFINITY || v != v ? 1u << (j & 31) : 0u;
-                    if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (all at once they cost registers of the whole loop)
-                }
-            }
-        }
-        if (!more) break;
-        tile = next;
-        next = next_but_one;
-    }
-    if (rescale) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[d][i] *= corr;
-    }
-    outputs_of(weights, buffer, 1);
-    bool any_inf = false;
-#pragma unroll
-    for (int w = 0; w < WORDS; ++w) any_inf |= (most_inf[w] | least_inf[w]) != 0u;
-    if (__any(any_inf)) {
-#pragma unroll
-        for (int j = 0; j < DT * 16; ++j) {
-            if (most_inf[j / 32] >> (j & 31) & 1u) acc[j >> 4][j & 15] += INFINITY;
-            if (least_inf[j / 32] >> (j & 31) & 1u) acc[j >> 4][j & 15] -= INFINITY;
-        }
-    }
-    write_rows<bf16, D>(p, span, hk, wave_row, rows, acc, top, shift, l);
+// Few rows leave the chip empty: below so many blocks of whole rows they are split, if there is more than a tile of 32 entries to split.  us,
+// whole and split, at the number of blocks - bf16, 128 values: 96 40.0 and 37.9, 128 42.3 and 48.3; 64 values: 280 16.1 and 14.3, 512 42.2 and 54.8; 32
+// values: 520 11.2 and 8.8, 1024 25.4 and 33.2.  fp32, 128 values: 192 156 and 94, 256 24.9 and 44.4 (of longer prompts 157 and 119); 64 values: 520
+// 51.0 and 33.1, 1024 162 and 181; 32 values: 520 31.5 and 17.5, 1024 96.9 and 88.0.
+int64_t split_below(int dtype, int D) {
+    if (dtype == PIKV_F32) return D == 128 ? 256 : D == 64 ? 640 : 1024;
+    return D == 128 ? 112 : D == 64 ? 320 : 640;
 }
 
 }  // namespace
@@ -631,9 +399,11 @@ extern "C" int pikv_prompt_attn(const void *q, const void *k, const void *v, int
     if ((row_max != nullptr) != (row_norm != nullptr)) return PIKV_ERR_INVALID;
     if (max_len > tokens) max_len = tokens;
     const int G = Hq / Hkv;
-    const int block_threads = dtype == PIKV_F32 ? kThreads : D == 32 ? staged_threads<32> : staged_threads<64>, block_rows = block_threads / 2;
-    static_assert(staged_threads<64> == staged_threads<128>, "as above");
-    const int64_t tiles = ((int64_t)max_len * G + block_rows - 1) / block_rows;
+    const int waves = (dtype == PIKV_F32 ? threads_of<float, 64> : D == 32 ? threads_of<bf16, 32> : threads_of<bf16, 64>) / kWave;
+    static_assert(threads_of<float, 32> == threads_of<float, 64> && threads_of<float, 64> == threads_of<float, 128> && threads_of<bf16, 64> == threads_of<bf16, 128>, "as above");
+    auto tiles_of = [&](int block_rows) { return ((int64_t)max_len * G + block_rows - 1) / block_rows; };
+    const bool split = max_len > 32 && (int64_t)B * Hkv * tiles_of(waves * kWaveRows) < split_below(dtype, D);
+    const int64_t tiles = tiles_of(split ? kWaveRows : waves * kWaveRows);
     if ((int64_t)B * Hkv * tiles >= (1 << 23)) return PIKV_ERR_UNSUPPORTED;
     if (tokens == 0 || B == 0 || max_len == 0) return PIKV_OK;       // (tensors without elements have no address)
     if (!q || !k || !v || !cu_seqlens || !out || reinterpret_cast<uintptr_t>(out) % 16 != 0) return PIKV_ERR_INVALID;
@@ -649,15 +419,15 @@ extern "C" int pikv_prompt_attn(const void *q, const void *k, const void *v, int
     p.by_head = fast_div(Hkv);
     p.by_tile = fast_div(B);
     p.tiles = (int)tiles;
-    const dim3 grid((unsigned)(B * Hkv * tiles)), threads(block_threads);
+    const dim3 grid((unsigned)(B * Hkv * tiles)), threads((split ? kSplitWaves : waves) * kWave);
     hipStream_t st = as_stream(stream);
     auto launch = [&](auto type, auto width) {
         typedef decltype(type) T;
         constexpr int W = decltype(width)::value;
         auto go = [&](auto capped, auto biased) {
             constexpr bool CAP = decltype(capped)::value, BIAS = decltype(biased)::value;
-            if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((prompt_attn_staged<W, CAP, BIAS>), grid, threads, 0, st, p);
-            else hipLaunchKernelGGL((prompt_attn<T, W, CAP, BIAS>), grid, threads, 0, st, p);
+            if (split) hipLaunchKernelGGL((prompt_attn<T, W, CAP, BIAS, true>), grid, threads, 0, st, p);
+            else hipLaunchKernelGGL((prompt_attn<T, W, CAP, BIAS, false>), grid, threads, 0, st, p);
         };
         const std::true_type yes{};
         const std::false_type no{};

@@ -115,6 +115,18 @@ def test_prompts_and_their_utilities(shape, mask, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mask", MASKS, ids=lambda m: "_".join(m) or "causal")
+@pytest.mark.parametrize("shape", [([70] * 30 + [300, 129], 16, 16, 128), ([70] * 30 + [133], 24, 24, 64), ([40] * 30 + [133], 40, 40, 32), ([20, 32, 1], 6, 2, 64)],
+                         ids=lambda s: "x%d_H%d_%d_D%d" % (len(s[0]), *s[1:]))
+def test_enough_prompts_for_blocks_of_many_rows_and_prompts_of_a_tile(shape, mask, dtype):
+    d = Device(Prompts(*shape, dtype, seed=21, **with_prefix(mask, shape[0])))
+    d.attend()
+    check_attention(d)
+    d.weigh()
+    check_mass(d)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_every_token_gives_each_head_one_unit_of_attention(dtype):
     p = Prompts([333, 90], 8, 4, 64, dtype, seed=4)
     d = Device(p)
@@ -168,24 +180,26 @@ def test_counts_that_leave_the_arrays_are_cut_off():
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D", [32, 64, 128])
-def test_what_is_not_seen_may_hold_anything(D, dtype):
-    """A token that holds NaN or infinities changes the rows that see it, and no other."""
-    clean = Prompts([150], 4, 2, D, dtype, seed=7, window=60, prefix=[4])
+@pytest.mark.parametrize("others", [0, 600], ids=["few", "many"])
+def test_what_is_not_seen_may_hold_anything(others, D, dtype):
+    """A token that holds NaN or infinities changes the rows that see it, and no other.  (With many short prompts beside: blocks of many rows.)"""
+    fresh = lambda: Prompts([150] + [2] * others, 4, 2, D, dtype, seed=7, window=60, prefix=[4] + [0] * others)
+    clean = fresh()
     ref = Device(clean)
     ref.attend()
     for bad in (np.nan, np.inf, -np.inf):
-        p = Prompts([150], 4, 2, D, dtype, seed=7, window=60, prefix=[4])
+        p = fresh()
         p.v[70, 0, 3] = bad
         d = Device(p)
         d.attend()
-        token = np.arange(150)
+        token = np.arange(clean.tokens)
         sees = (token >= 70) & (token - 70 < 60)
         got, want = host(d.out), host(ref.out)
         touched = np.zeros(got.shape, bool)
         touched[sees, :2, 3] = True
         np.testing.assert_array_equal(got[~touched], want[~touched])
         assert (np.isnan(got[touched]) if np.isnan(bad) else got[touched] == bad).all()
-        p = Prompts([150], 4, 2, D, dtype, seed=7, window=60, prefix=[4])
+        p = fresh()
         p.k[70, 1] = bad
         d = Device(p)
         d.attend()
@@ -194,7 +208,7 @@ def test_what_is_not_seen_may_hold_anything(D, dtype):
         touched[sees, 2:] = True
         np.testing.assert_array_equal(got[~touched], want[~touched])
     # a query: its own rows only, and the entries it sees
-    p = Prompts([150], 4, 2, D, dtype, seed=7, window=60, prefix=[4])
+    p = fresh()
     p.q[100, 1] = np.nan
     d = Device(p)
     d.attend()
@@ -203,11 +217,11 @@ def test_what_is_not_seen_may_hold_anything(D, dtype):
     got[100, 1] = want[100, 1]
     np.testing.assert_array_equal(got, want)
     d.weigh()
-    token = np.arange(150)
+    token = np.arange(clean.tokens)
     assert np.isnan(host(d.mass)[(token > 40) & (token <= 100)]).all()
     ref.weigh()
-    others = ~(((token > 40) & (token <= 100)) | (token < 4))
-    np.testing.assert_array_equal(host(d.mass)[others], host(ref.mass)[others])
+    rest = ~(((token > 40) & (token <= 100)) | (token < 4))
+    np.testing.assert_array_equal(host(d.mass)[rest], host(ref.mass)[rest])
 
 
 def test_scores_beyond_the_range_of_their_cap():
