@@ -17,17 +17,16 @@ namespace pikv {
 namespace {
 
 constexpr int kWaveRows = 32;            // rows of a wave
-// bf16 rows of 64 values and more: 8 waves, as a tile's way into LDS takes a sixth of the time of 4.  (fp32: matrix instructions of four times the
-// length; rows of 32 values: a tile is 256 pieces.)
-template <typename T, int D>
-constexpr int threads_of = sizeof(T) == 2 && D >= 64 ? 512 : 256;
+// Waves of a block of many rows.  (8 waves halve the way of a tile into LDS for each row, and wait for each other: 16384 tokens of 128 values 2269 us
+// against 2325, of 64 values 1681 against 1363, 16 x 1024 tokens 240 against 219, ragged prompts in a window 167 against 153.)
+constexpr int kWaves = 4;
 
 // LDS tiles of KEYS entries x D values, in 16-byte chunks, a row's chunks exchanged by an xor so that the reads of a wave spread over
 // the banks: K is read as one chunk of 32 entries each, V (bf16) as 64 bytes of 4 neighbouring entries each.
 template <typename T, int D, bool SPLIT>
 struct Tile {
     static constexpr int KEYS = sizeof(T) == 2 && !SPLIT ? 64 : 32;
-    static constexpr int THREADS = SPLIT ? kWave : threads_of<T, D>;  // that bring a tile
+    static constexpr int THREADS = SPLIT ? kWave : kWaves * kWave;    // that bring a tile
     static constexpr int CHUNKS = D * (int)sizeof(T) / 16;            // of a row
     static constexpr int PER_THREAD = KEYS * CHUNKS / THREADS;        // of a tile
     static constexpr int PER_LINE = CHUNKS >= 16 ? 1 : 16 / CHUNKS;   // rows of 256 bytes
@@ -45,24 +44,18 @@ __device__ __forceinline__ uint2 read_transposed(const void *at) {
 
 // CAP: scores capped by a tanh; BIAS: with a distance term.  SPLIT: for few rows, a block takes 32 of them and its waves every fourth tile each, by
 // themselves; their results are joined at the end.
-constexpr int kSplitWaves = 4;
-template <typename T, int D, bool SPLIT>
-constexpr int block_waves = SPLIT ? kSplitWaves : threads_of<T, D> / kWave;
 template <typename T, int D, bool CAP, bool BIAS, bool SPLIT>
-__global__ __launch_bounds__((block_waves<T, D, SPLIT> * kWave), (SPLIT && D == 128 ? 1 : 2)) void prompt_attn(PromptParams p) {
+__global__ __launch_bounds__(kWaves *kWave, (SPLIT && D == 128 ? 1 : 2)) void prompt_attn(PromptParams p) {
     typedef Tile<T, D, SPLIT> L;
-    constexpr int WAVES = block_waves<T, D, SPLIT>, ROWS = SPLIT ? kWaveRows : WAVES * kWaveRows, THREADS = L::THREADS;
+    constexpr int WAVES = kWaves, ROWS = SPLIT ? kWaveRows : WAVES * kWaveRows, THREADS = L::THREADS;
     constexpr bool BF = sizeof(T) == 2;
     constexpr int KEYS = L::KEYS, KB = KEYS / 32, DT = D / 32, BUFFERS = SPLIT ? WAVES : 2, STEP = SPLIT ? WAVES : 1;
     constexpr int QN = D * (int)sizeof(T) / 32;                       // 16-byte pieces of a lane's query
     __shared__ __attribute__((aligned(16))) uint4 Ks[BUFFERS][KEYS * L::CHUNKS], Vs[BUFFERS][KEYS * L::CHUNKS];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, h = lane >> 5;
-    // the blocks with the most entries first
     int hk, b;
-    const int rest = fast_divide(p.by_head, blockIdx.x, &hk);
-    int at_tile = fast_divide(p.by_tile, rest, &b);                   // (by_tile: sequences)
-    at_tile = p.tiles - 1 - at_tile;
+    const int at_tile = prompt_block(p, blockIdx.x, true, &hk, &b);      // (the blocks with the most entries first)
     const Span span = prompt_span(p, b);
     const int n = span.n, rows = n * p.G, row0 = at_tile * ROWS;
     if (row0 >= rows) return;
@@ -376,13 +369,15 @@ __global__ __launch_bounds__((block_waves<T, D, SPLIT> * kWave), (SPLIT && D == 
     }
 }
 
-// Few rows leave the chip empty: below so many blocks of whole rows they are split, if there is more than a tile of 32 entries to split.  us,
-// whole and split, at the number of blocks - bf16, 128 values: 96 40.0 and 37.9, 128 42.3 and 48.3; 64 values: 280 16.1 and 14.3, 512 42.2 and 54.8; 32
-// values: 520 11.2 and 8.8, 1024 25.4 and 33.2.  fp32, 128 values: 192 156 and 94, 256 24.9 and 44.4 (of longer prompts 157 and 119); 64 values: 520
-// 51.0 and 33.1, 1024 162 and 181; 32 values: 520 31.5 and 17.5, 1024 96.9 and 88.0.
-int64_t split_below(int dtype, int D) {
-    if (dtype == PIKV_F32) return D == 128 ? 256 : D == 64 ? 640 : 1024;
-    return D == 128 ? 112 : D == 64 ? 320 : 640;
+// Few rows leave the chip empty: up to so many blocks of whole rows they are split instead, if there is more than a tile of 32 entries to split; of
+// prompts of up to 128 tokens, which have little to split, up to a third of that.  us, whole and split, at a number of blocks (prompts) -
+// bf16, 128 values: 128 (2048) 59.5 and 38.3, 160 (400) 16.6 and 15.2, 192 (1000) 34.6 and 38.6, 48 (100) 9.9 and 8.1, 96 (100) 10.1 and 14.1;
+// 64 values: 256 (1024) 26.4 and 19.6, 512 (1000) 28.3 and 30.6, 128 (100) 7.7 and 6.9, 256 (100) 8.3 and 10.0; 32 values: 512 (1000) 22.2 and 19.8,
+// 512 (500) 13.3 and 14.1.  fp32, 128 values: 256 (1024) 156 and 118, 512 (2048) 395 and 394, 256 (100) 24.9 and 44.4; 64 values: 520 (400) 51.0 and 33.1,
+// 1024 (1000) 162 and 181, 256 (100) 15.1 and 18.8; 32 values: 1024 (1000) 96.9 and 88.0.
+bool splits(int dtype, int D, int max_len, int64_t blocks) {
+    const int64_t most = dtype == PIKV_F32 ? (D == 128 ? 300 : D == 64 ? 640 : 1024) : (D == 128 ? 176 : D == 64 ? 400 : 560);
+    return max_len > 32 && blocks <= (max_len > 128 ? most : most / 3);
 }
 
 }  // namespace
@@ -399,11 +394,9 @@ extern "C" int pikv_prompt_attn(const void *q, const void *k, const void *v, int
     if ((row_max != nullptr) != (row_norm != nullptr)) return PIKV_ERR_INVALID;
     if (max_len > tokens) max_len = tokens;
     const int G = Hq / Hkv;
-    const int waves = (dtype == PIKV_F32 ? threads_of<float, 64> : D == 32 ? threads_of<bf16, 32> : threads_of<bf16, 64>) / kWave;
-    static_assert(threads_of<float, 32> == threads_of<float, 64> && threads_of<float, 64> == threads_of<float, 128> && threads_of<bf16, 64> == threads_of<bf16, 128>, "as above");
     auto tiles_of = [&](int block_rows) { return ((int64_t)max_len * G + block_rows - 1) / block_rows; };
-    const bool split = max_len > 32 && (int64_t)B * Hkv * tiles_of(waves * kWaveRows) < split_below(dtype, D);
-    const int64_t tiles = tiles_of(split ? kWaveRows : waves * kWaveRows);
+    const bool split = splits(dtype, D, max_len, (int64_t)B * Hkv * tiles_of(kWaves * kWaveRows));
+    const int64_t tiles = tiles_of(split ? kWaveRows : kWaves * kWaveRows);
     if ((int64_t)B * Hkv * tiles >= (1 << 23)) return PIKV_ERR_UNSUPPORTED;
     if (tokens == 0 || B == 0 || max_len == 0) return PIKV_OK;       // (tensors without elements have no address)
     if (!q || !k || !v || !cu_seqlens || !out || reinterpret_cast<uintptr_t>(out) % 16 != 0) return PIKV_ERR_INVALID;
@@ -419,7 +412,7 @@ extern "C" int pikv_prompt_attn(const void *q, const void *k, const void *v, int
     p.by_head = fast_div(Hkv);
     p.by_tile = fast_div(B);
     p.tiles = (int)tiles;
-    const dim3 grid((unsigned)(B * Hkv * tiles)), threads((split ? kSplitWaves : waves) * kWave);
+    const dim3 grid((unsigned)(B * Hkv * tiles)), threads(kWaves * kWave);
     hipStream_t st = as_stream(stream);
     auto launch = [&](auto type, auto width) {
         typedef decltype(type) T;

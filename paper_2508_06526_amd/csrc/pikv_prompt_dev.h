@@ -31,6 +31,20 @@ __device__ __forceinline__ int row_token(const PromptParams &p, int row) {
     return t;
 }
 
+// What block `id` takes: its tile (0 .. tiles - 1; counted down for `last_first`), kv head and sequence.  Blocks go to the XCDs in turn, so
+// that the heads of a sequence stay on one where there are 8; the sequences are turned by one from tile to tile, or where there are fewer
+// heads an XCD would get all blocks of a long one (4 ragged prompts of up to 4001 tokens, 4 kv heads: 275 us
+// without turning them, 183 with).
+__device__ __forceinline__ int prompt_block(const PromptParams &p, int id, bool last_first, int *hk, int *b) {
+    id = fast_divide(p.by_head, id, hk);
+    int tile = fast_divide(p.by_tile, id, b), turn;              // (by_tile: sequences)
+    if (last_first) tile = p.tiles - 1 - tile;
+    fast_divide(p.by_tile, tile, &turn);
+    *b += turn;
+    if (*b >= p.B) *b -= p.B;
+    return tile;
+}
+
 struct Span {
     int first, n;                        // the sequence's rows; n: those below max_len
 };

@@ -39,9 +39,8 @@ __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, h = lane >> 5;
     int hk, b, split;
-    int id = fast_divide(p.by_head, blockIdx.x, &hk);
-    id = fast_divide(p.by_split, id, &split);
-    const int at_tile = fast_divide(p.by_tile, id, &b);               // the entries with the most rows first
+    const int id = fast_divide(p.by_split, blockIdx.x, &split);      // (a block's runs: on one XCD after the other)
+    const int at_tile = prompt_block(p, id, false, &hk, &b);         // the entries with the most rows first
     const Span span = prompt_span(p, b);
     const int n = span.n, entry0 = at_tile * kWaves * ENTRIES;
     if (entry0 >= n) return;
