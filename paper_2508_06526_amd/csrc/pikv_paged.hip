@@ -1,7 +1,7 @@
 // Writing a paged cache: the rows of whole prompts, and a step's entry.
 //
 //   fill_plan    : a block per shard gives the tokens that selected it their slots.  Every wave counts those of a run of tokens by
-//                  ballots; one scan over the waves, and a second walk writes the slots.  Where the shard has too little room, a radix
+//                  ballots, the tokens in registers; one scan over the waves, and a second walk writes the slots.  Where the shard has too little room, a radix
 //                  select over the weights (3 rounds of 11, 11 and 10 bits, counts in LDS: any order of its atomics gives the
 //                  same) finds the cut first.
 //   fill_rows    : lanes take the 16-byte pieces of a token's rows and write them to each of its slots: every row is read once.
@@ -25,13 +25,17 @@ struct FillParams {
 };
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / kWave;
-constexpr int kPlanAhead = 4;                    // tokens of a lane whose selections are requested together
-constexpr int kBins = 2048;
+constexpr int kHeld = 16;                        // tokens of a lane that it asks for together, and keeps if the sequence has no more (16384)
+constexpr int kBins = 2 * kPlanThreads;          // of a round of the select
 
-// The place of expert e in a token's selection: the first of them, -1 if there is none.
+// The place of expert e in a token's selection: the first of them, -1 if there is none.  (The first four are requested together.)
 __device__ __forceinline__ int place_of(const int32_t *topk, int k, int e) {
-    int at = -1;
-    for (int j = k - 1; j >= 0; --j) at = topk[j] == e ? j : at;
+    int listed[4], at = -1;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) listed[j] = topk[min(j, k - 1)];
+    for (int j = k - 1; j >= 4; --j) at = topk[j] == e ? j : at;
+#pragma unroll
+    for (int j = 3; j >= 0; --j) at = listed[j] == e && j < k ? j : at;
     return at;
 }
 
@@ -39,40 +43,50 @@ __device__ __forceinline__ uint32_t weight_key(float w) { return w != w ? 0u : o
 
 __global__ __launch_bounds__(kPlanThreads) void fill_plan(FillParams p) {
     __shared__ int hist[kBins];
-    __shared__ int above[kPlanWaves], ties[kPlanWaves], found[3], first_missing;
+    __shared__ int above[kPlanWaves], ties[kPlanWaves], sums[kPlanWaves], found[2], first_missing;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t be = blockIdx.x;
     const int b = blockIdx.x / p.E, e = blockIdx.x - b * p.E;
     const int lo = min(max(p.cu[b], 0), p.tokens), hi = min(max(p.cu[b + 1], lo), p.tokens);
     const int n = p.n_valid[be];
+    hist[tid] = hist[tid + kPlanThreads] = 0;
     if (tid == 0) first_missing = p.pages.per_shard;
+    // a wave's tokens: a run of whole steps
+    const int steps = (hi - lo + kPlanThreads - 1) / kPlanThreads, from = lo + wave * steps * kWave, to = min(hi, from + steps * kWave);
+    int place[kHeld], position[kHeld];
+    float weight[kHeld];
+    auto fetch = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+            if (t0 + u * kWave < to) {           // (uniform)
+                const int t = min(t0 + u * kWave + lane, to - 1);
+                place[u] = place_of(p.topk + (int64_t)t * p.k, p.k, e);
+                weight[u] = p.weight ? p.weight[t] : 0.0f;
+                position[u] = p.entry_pos ? p.positions[t] : 0;
+                if (t0 + u * kWave + lane >= to) place[u] = -1;
+            } else {
+                place[u] = -1;
+            }
+            if (u % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (all addresses at once cost registers)
+        }
+    };
+    const bool once = steps <= kHeld;
+    if (once) fetch(from);
+    auto walk = [&](auto visit) __attribute__((always_inline)) {                // visit(token, place, weight, position), in order, all lanes of the wave together
+        for (int t0 = from; t0 < to; t0 += kHeld * kWave) {
+            if (!once) fetch(t0);
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u)
+                if (t0 + u * kWave < to) visit(t0 + u * kWave + lane, place[u], weight[u], position[u]);
+        }
+    };
     __syncthreads();
-    const int held_pages = max(n, 0) >> p.pages.bits;
-    for (int i = held_pages + tid; i < p.pages.per_shard; i += kPlanThreads) {
+    for (int i = (max(n, 0) >> p.pages.bits) + tid; i < p.pages.per_shard; i += kPlanThreads) {
         const int page = p.pages.table[be * p.pages.per_shard + i];
         if (page < 0 || page >= p.pages.n_pages) atomicMin(&first_missing, i);
     }
-    // a wave's tokens: a run of whole steps
-    const int steps = (hi - lo + kPlanThreads - 1) / kPlanThreads, from = lo + wave * steps * kWave, to = min(hi, from + steps * kWave);
-    auto walk = [&](auto weighted, auto visit) {         // visit(token, place or -1, key), in order, all lanes of the wave together
-        for (int t0 = from; t0 < to; t0 += kPlanAhead * kWave) {
-            int place[kPlanAhead];
-            float w[kPlanAhead];
-#pragma unroll
-            for (int u = 0; u < kPlanAhead; ++u) {
-                const int t = min(t0 + u * kWave + lane, to - 1);
-                place[u] = place_of(p.topk + (int64_t)t * p.k, p.k, e);
-                w[u] = weighted.value ? p.weight[t] : 0.0f;
-            }
-#pragma unroll
-            for (int u = 0; u < kPlanAhead; ++u) {
-                const int t = t0 + u * kWave + lane;
-                visit(t, t < to ? place[u] : -1, weighted.value ? weight_key(w[u]) : 0u);
-            }
-        }
-    };
     int mine = 0;
-    walk(std::false_type{}, [&](int, int place, uint32_t) { mine += __popcll(__ballot(place >= 0)); });
+    walk([&](int, int at, float, int) { mine += __popcll(__ballot(at >= 0)); });
     if (lane == 0) above[wave] = 0, ties[wave] = mine;
     __syncthreads();
     const int64_t room_end = min((int64_t)p.S, (int64_t)first_missing << p.pages.bits);
@@ -86,32 +100,30 @@ __global__ __launch_bounds__(kPlanThreads) void fill_plan(FillParams p) {
         uint32_t prefix = 0;
         if (room == 0) cut = 0xffffffffu;
         else {
-#pragma unroll
             for (int round = 0; round < 3; ++round) {
                 const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
-                for (int i = tid; i < kBins; i += kPlanThreads) hist[i] = 0;
-                __syncthreads();
-                walk(std::true_type{}, [&](int, int place, uint32_t key) {
+                walk([&](int, int place, float weight, int) {
+                    const uint32_t key = weight_key(weight);
                     const bool in = round == 0 || (key >> (shift + bits)) == prefix;
                     if (place >= 0 && in) atomicAdd(&hist[(key >> shift) & ((1 << bits) - 1)], 1);
                 });
                 __syncthreads();
-                if (wave == 0) {         // bins from the top: lane l takes a run, then the lanes' sums
-                    const int per = (1 << bits) / kWave, top = (1 << bits) - 1 - lane * per;
-                    int sum = 0;
-                    for (int i = 0; i < per; ++i) sum += hist[top - i];
-                    int before = sum;
-                    for (int off = 1; off < kWave; off <<= 1) {
-                        const int other = __shfl_up(before, off, kWave);
-                        if (lane >= off) before += other;
-                    }
-                    before -= sum;
-                    if (before < want && want <= before + sum) {     // one lane
-                        int bin = top;
-                        while (before + hist[bin] < want) before += hist[bin--];
-                        found[0] = bin;
-                        found[1] = before;
-                    }
+                // bins from the top, two a thread; counts above them: of the lanes, then the waves, before
+                const int top = kBins - 1 - 2 * tid, first = hist[top], both = first + hist[top - 1];
+                hist[top] = hist[top - 1] = 0;
+                int incl = both;
+                for (int off = 1; off < kWave; off <<= 1) {
+                    const int other = __shfl_up(incl, off, kWave);
+                    if (lane >= off) incl += other;
+                }
+                if (lane == kWave - 1) sums[wave] = incl;
+                __syncthreads();
+                int before = incl - both;
+                for (int w = 0; w < wave; ++w) before += sums[w];
+                if (before < want && want <= before + both) {            // one thread
+                    const bool second = want > before + first;
+                    found[0] = second ? top - 1 : top;
+                    found[1] = second ? before + first : before;
                 }
                 __syncthreads();
                 prefix = (prefix << bits) | (uint32_t)found[0];
@@ -119,12 +131,13 @@ __global__ __launch_bounds__(kPlanThreads) void fill_plan(FillParams p) {
             }
             cut = prefix;
         }
-        __syncthreads();                 // every wave has read the counts
         int over = 0, at = 0;
-        walk(std::true_type{}, [&](int, int place, uint32_t key) {
+        walk([&](int, int place, float weight, int) {
+            const uint32_t key = weight_key(weight);
             over += __popcll(__ballot(place >= 0 && key > cut));
             at += __popcll(__ballot(place >= 0 && key == cut));
         });
+        __syncthreads();                 // every wave has read the counts
         if (lane == 0) above[wave] = over, ties[wave] = at;
         __syncthreads();
     }
@@ -135,24 +148,21 @@ __global__ __launch_bounds__(kPlanThreads) void fill_plan(FillParams p) {
     }
     const int of_ties = room - all_over;         // at the cut: this many stay
     const uint64_t before_lane = (1ull << lane) - 1;
-    auto place_tokens = [&](auto weighted) {
-        walk(weighted, [&](int t, int place, uint32_t key) {
-            const bool is_over = weighted.value && place >= 0 && key > cut, is_at = place >= 0 && (!weighted.value || key == cut);
-            const uint64_t over_votes = __ballot(is_over), at_votes = __ballot(is_at);
-            const int my_over = over + __popcll(over_votes & before_lane), my_at = at + __popcll(at_votes & before_lane);
-            over += __popcll(over_votes);
-            at += __popcll(at_votes);
-            if (place < 0) return;
-            const bool stays = is_over || (is_at && my_at < of_ties);
-            const int slot = stays ? n + my_over + min(my_at, of_ties) : -1;
-            p.slots[(int64_t)t * p.k + place] = slot;
-            if (!stays) return;
-            p.utility[be * p.S + slot] = p.weight ? p.weight[t] : 0.0f;
-            if (p.entry_pos) p.entry_pos[be * p.S + slot] = p.positions[t];
-        });
-    };
-    if (chosen) place_tokens(std::true_type{});
-    else place_tokens(std::false_type{});
+    walk([&](int t, int place, float weight, int position) {
+        const uint32_t key = weight_key(weight);
+        const bool is_over = chosen && place >= 0 && key > cut, is_at = place >= 0 && (!chosen || key == cut);
+        const uint64_t over_votes = __ballot(is_over), at_votes = __ballot(is_at);
+        const int my_over = over + __popcll(over_votes & before_lane), my_at = at + __popcll(at_votes & before_lane);
+        over += __popcll(over_votes);
+        at += __popcll(at_votes);
+        if (place < 0) return;
+        const bool stays = is_over || (is_at && my_at < of_ties);
+        const int slot = stays ? n + my_over + min(my_at, of_ties) : -1;
+        p.slots[(int64_t)t * p.k + place] = slot;
+        if (!stays) return;
+        p.utility[be * p.S + slot] = weight;
+        if (p.entry_pos) p.entry_pos[be * p.S + slot] = position;
+    });
     if (tid == 0 && min(total, room) > 0) p.n_valid[be] = n + min(total, room);
 }
 
