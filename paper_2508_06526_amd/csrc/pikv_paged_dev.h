@@ -17,8 +17,9 @@ inline int check_paged(const pikv_desc *d, const pikv_pages *pages) {
     if (pages->n_pages < 1) return PIKV_ERR_INVALID;
     if (pages->page != 16 && pages->page != 32 && pages->page != 64 && pages->page != 128 && pages->page != 256) return PIKV_ERR_INVALID;
     const int64_t es = elem_bytes(d->dtype), D = d->D, sp = pages->stride_page, sh = pages->stride_h, ss = pages->stride_s;
-    if (sp <= 0 || sh < 0 || ss < D || sp * es % 16 != 0 || sh * es % 16 != 0 || ss * es % 16 != 0) return PIKV_ERR_INVALID;
-    if (ss * es > (1 << 24) || sh > ((int64_t)1 << 40) || sp > ((int64_t)1 << 40)) return PIKV_ERR_UNSUPPORTED;
+    if (sp <= 0 || sh < 0 || ss < D) return PIKV_ERR_INVALID;
+    if (ss > (1 << 24) / es || sh > ((int64_t)1 << 40) || sp > ((int64_t)1 << 40)) return PIKV_ERR_UNSUPPORTED;
+    if (sp * es % 16 != 0 || sh * es % 16 != 0 || ss * es % 16 != 0) return PIKV_ERR_INVALID;
     // no two rows overlap: the rows of a head one behind the other, or the heads of a slot
     const int64_t rows = (int64_t)(pages->page - 1) * ss + D, heads = (int64_t)(d->Hkv - 1) * sh + D;
     if (d->Hkv > 1 && sh < rows && (sh < D || ss < heads)) return PIKV_ERR_INVALID;

@@ -81,7 +81,8 @@ inline int check_prompt(const void *q, const void *k, const void *v, bool values
         return stride >= (int64_t)heads * D && stride * es % 16 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
     };
     // (64 rows are addressed with 32 bits)
-    if (q_stride * es > (1 << 25) || k_stride * es > (1 << 25) || (values && v_stride * es > (1 << 25))) return PIKV_ERR_UNSUPPORTED;
+    const int64_t most = (1 << 25) / es;
+    if (q_stride > most || k_stride > most || (values && v_stride > most)) return PIKV_ERR_UNSUPPORTED;
     if (!rows(q, q_stride, Hq) || !rows(k, k_stride, Hkv) || (values && !rows(v, v_stride, Hkv))) return PIKV_ERR_INVALID;
     return PIKV_OK;
 }

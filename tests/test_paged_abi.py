@@ -169,3 +169,20 @@ def test_the_binding_refuses_host_memory_and_other_types(name):
         calls[name](i32, f(4, t=torch.float64))
     with pytest.raises(TypeError):
         calls[name](i32, f(4), f(16, t=torch.float16))
+
+
+@pytest.mark.parametrize("call", [prompt, mass], ids=["attention", "mass"])
+def test_strides_and_lengths_beyond_the_offsets_of_the_kernels(lib, call):
+    """A row's stride of 2^25 bytes is the largest; none wraps around to one that fits."""
+    names = ["q_stride", "k_stride"] + (["v_stride"] if call is prompt else [])
+    for name in names:
+        assert call(lib, **{name: (1 << 24) + 8}) == UNSUPPORTED
+        assert call(lib, dtype=0, **{name: (1 << 23) + 4}) == UNSUPPORTED
+        assert call(lib, **{name: 1 << 62}) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("name", ["stride_s", "stride_h", "stride_page"])
+def test_strides_of_pages_beyond_the_offsets_of_the_kernels(lib, name):
+    for value in (1 << 41, 1 << 61, 1 << 62):
+        args = [FAKE] * 3, [2], [FAKE] * 2, [1], [FAKE] * 7, [None]
+        assert lib.pikv_paged_append(*given(dict(g={"stride_page": 1 << 20, name: value})), *sum(args, [])) == UNSUPPORTED
