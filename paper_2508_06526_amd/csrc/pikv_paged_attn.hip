@@ -527,9 +527,19 @@ int make_plan(const pikv_desc *d, int k, bool positions, PagedPlan *plan) {
     plan->rows = per_head ? 1 : G < plan->row_tiles * kRows ? G : plan->row_tiles * kRows;
     plan->row_blocks = (G + plan->rows - 1) / plan->rows;
     const int64_t units = (int64_t)d->B * d->Hkv * plan->row_blocks * k;
-    const int64_t blocks = units / k, rows = (int64_t)k * d->S;
-    const bool one_round = (int64_t)d->S * (d->D > 64 ? d->D : 64) <= (int64_t)128 * stage * (kMergedWaves / k);
-    plan->merged = plan->row_tiles == 1 && k <= kMergedWaves && blocks <= 640 && (one_round || (blocks >= 192 && rows <= 4096));
+    // One launch or two.  One: where a block's waves get a stage each, and where its blocks, one on a CU, fill the CUs' rounds - 9 of 10 of
+    // them, or 3 of 4 of a single one - with up to 4096 (1024) rows each; then the second launch and the partials cost more than blocks
+    // of unequal length.  us, in one launch and in two, 8 kv heads of 4 rows, bf16, 2 shards of S full slots:
+    //   128 values, S = 64 / 128:               8 blocks 6.3 : 7.4,  7.4 : 7.9;     192 blocks 6.6 : 9.6,  8.5 : 11.3
+    //   128 values, S = 512 / 1024 / 2048:      192 blocks 22 : 26,  40 : 44,  75 : 68;     256 blocks 24 : 28,  44 : 46,  85 : 90;
+    //                                           320 blocks 41 : 37,  74 : 62,  142 : 113;   640 blocks 67 : 64,  123 : 113,  235 : 221;
+    //                                           1024 blocks 98 : 96,  173 : 179,  336 : 356
+    //   shards of 0 .. S slots, 256 blocks:     19 : 22,  35 : 39,  66 : 66;   S = 4096: 114 : 99
+    //   4 shards, with positions, 192 blocks:   S = 256  24 : 24,  512  44 : 39;   fp32, 640 blocks: S = 256  81 : 70
+    const int64_t blocks = units / k, rows = (int64_t)k * d->S, places = (blocks + 255) / 256 * 256;
+    const bool one_round = blocks <= 640 && (int64_t)d->S * (d->D > 64 ? d->D : 64) <= (int64_t)128 * stage * (kMergedWaves / k);
+    const bool filled = blocks <= 1024 && ((10 * blocks >= 9 * places && rows <= 4096) || (blocks >= 192 && blocks <= 256 && rows <= 1024));
+    plan->merged = plan->row_tiles == 1 && k <= kMergedWaves && (one_round || filled);
     // A block per CU, and blocks of at most 1024 rows, but none of fewer than a stage of each wave.
     int64_t nsplit = units > 0 ? 256 / units : 1;
     const int64_t finer = (d->S + kLongestBlock - 1) / kLongestBlock, most = (d->S + kWaves * stage - 1) / (kWaves * stage);
