@@ -105,7 +105,10 @@ __global__ __launch_bounds__(kWaves *kWave, (SPLIT && D == 128 ? 1 : 2)) void pr
 #pragma unroll
             for (int u = 0; u < L::PER_THREAD; ++u)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) bad |= special(vr[u][i]) || (BF && special(vr[u][i] << 16));
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t w = opaque(vr[u][i]);     // (else its masking, which the branch below has too, is done for every tile)
+                    bad |= special(w) || (BF && special(w << 16));
+                }
         }
         // pieces tid, tid + THREADS, ..: the exchange of rows tid / CHUNKS + u LINES is that of either
         constexpr int LINES = THREADS / L::CHUNKS;
