@@ -22,7 +22,8 @@ struct QTile {
     static constexpr int ROWS = 64;
     static constexpr int CHUNKS = D * (int)sizeof(T) / 16, PER_THREAD = ROWS * CHUNKS / kThreads;
     static constexpr int PER_LINE = CHUNKS >= 16 ? 1 : 16 / CHUNKS;
-    static __device__ __forceinline__ int chunk(int row, int c) { return row * CHUNKS + (c ^ ((row / PER_LINE) & (CHUNKS < 16 ? CHUNKS - 1 : 15))); }
+    static constexpr __device__ __forceinline__ int exchange(int row) { return (row / PER_LINE) & (CHUNKS < 16 ? CHUNKS - 1 : 15); }
+    static __device__ __forceinline__ int chunk(int row, int c) { return row * CHUNKS + (c ^ exchange(row)); }
 };
 
 // CAP: scores capped by a tanh; BIAS: with a distance term.
@@ -68,29 +69,37 @@ __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
     uint4 qr[L::PER_THREAD];
     float max_r = 0.0f, norm_r = 0.0f, slope_r = 0.0f;
     int token_r = 0;
+    // Rows row0 .. of the block's run, as they lie from the first one's token on: 32-bit offsets, and quotients of small numbers, for which the
+    // reciprocal is exact.
+    const uint32_t q_bytes = (uint32_t)p.q_stride * (uint32_t)sizeof(T), turn_bytes = q_bytes - p.G * D * (uint32_t)sizeof(T);
     auto request = [&](int row0) {
         const int tid = (int)opaque(threadIdx.x);
+        const int token0 = row_token(p, row0), phase = row0 - token0 * p.G, last = min(ROWS, to - row0) - 1;
+        const char *base = static_cast<const char *>(p.q) + ((int64_t)(span.first + token0) * p.q_stride + (int64_t)hk * p.G * D) * (int64_t)sizeof(T);
+        auto token_of = [&](uint32_t row) { return p.G == 1 ? row : __umulhi(row, p.G_rcp); };
 #pragma unroll
         for (int u = 0; u < L::PER_THREAD; ++u) {
-            const int at = tid + u * kThreads, row = min(row0 + at / L::CHUNKS, to - 1), token = row_token(p, row), head = hk * p.G + row - token * p.G;
-            qr[u] = load16(static_cast<const char *>(p.q) + ((int64_t)(span.first + token) * p.q_stride + head * D) * (int64_t)sizeof(T) + (at % L::CHUNKS) * 16);
+            const uint32_t row = min(tid / L::CHUNKS + u * (kThreads / L::CHUNKS), last) + phase;
+            qr[u] = load16(base + (token_of(row) * turn_bytes + row * (D * (uint32_t)sizeof(T)) + tid % L::CHUNKS * 16u));
         }
         if (tid < ROWS) {
-            const int row = min(row0 + tid, to - 1), head = hk * p.G + row - row_token(p, row) * p.G;
-            token_r = row_token(p, row);
-            const int64_t at = (int64_t)(span.first + token_r) * p.Hq + head;
-            max_r = p.row_max[at];
-            norm_r = row0 + tid < to ? p.row_norm[at] : 0.0f;
-            if constexpr (BIAS) slope_r = p.slopes[head];
+            const uint32_t row = min(tid, last) + phase, token = token_of(row), head = row - token * p.G;
+            const int64_t first = (int64_t)(span.first + token0) * p.Hq + hk * p.G;
+            const uint32_t at = token * p.Hq + head;
+            token_r = token0 + token;
+            max_r = p.row_max[first + at];
+            norm_r = tid <= last ? p.row_norm[first + at] : 0.0f;
+            if constexpr (BIAS) slope_r = p.slopes[hk * p.G + head];
         }
     };
     auto place = [&](int buffer) {
         const int tid = (int)opaque(threadIdx.x);
+        // (rows tid / CHUNKS + u LINES: their exchange is that of either)
+        constexpr int LINES = kThreads / L::CHUNKS;
+        const uint32_t at = L::chunk(tid / L::CHUNKS, tid % L::CHUNKS) * 16 + buffer * (int)sizeof(Qs[0]);
 #pragma unroll
-        for (int u = 0; u < L::PER_THREAD; ++u) {
-            const int at = tid + u * kThreads;
-            Qs[buffer][L::chunk(at / L::CHUNKS, at % L::CHUNKS)] = qr[u];
-        }
+        for (int u = 0; u < L::PER_THREAD; ++u)
+            *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(Qs) + ((at ^ (L::exchange(u * LINES) * 16)) + u * kThreads * 16)) = qr[u];
         if (tid < ROWS) {
             row_max_s[buffer][tid] = norm_r == 0.0f ? INFINITY : max_r;
             weight_s[buffer][tid] = norm_r == 0.0f ? 0.0f : 1.0f / norm_r;
