@@ -494,9 +494,11 @@ int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t block, const 
  *   prefix    [B] int32 or NULL;  slopes [Hq] float32 or NULL
  *   out       [tokens, Hq, D] dtype out: rows go on into a projection of the storage type
  *   row_max, row_norm [tokens, Hq] float32 out or both NULL: the largest score of the row and sum_j exp(s_j - row_max)
- * Errors: INVALID for null required pointers, one of row_max and row_norm without the other, tokens, B or max_len < 0, Hq or Hkv < 1, Hq % Hkv != 0, strides or
- * addresses as above, cap < 0, cap or scale NaN or infinite, unknown dtype; UNSUPPORTED for D other than 32, 64, 128, Hq > 256, tokens > 2^23 or 2^23
- * blocks of work and more (128 rows of a kv head's queries each).  tokens == 0, B == 0 and max_len == 0 are no-ops. */
+ * Errors: INVALID for null required pointers, one of row_max and row_norm without the other, tokens, B or max_len < 0, Hq or
+ * Hkv < 1, Hq % Hkv != 0, strides or
+ * addresses as above, cap < 0, cap or scale NaN or infinite, unknown dtype; UNSUPPORTED for D other than 32, 64, 128, Hq > 256, a
+ * stride above 2^25 bytes, tokens > 2^23 or 2^23 blocks of work and more (128 rows of a kv head's queries each, B times those of the
+ * longest sequence).  tokens == 0, B == 0 and max_len == 0 are no-ops.                                                 */
 int pikv_prompt_attn(const void *q, const void *k, const void *v, int32_t tokens, int64_t q_stride, int64_t k_stride,
                      int64_t v_stride, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype, const int32_t *cu_seqlens, int32_t B,
                      int32_t max_len, const int32_t *prefix, float scale, float cap, const float *slopes, int32_t window, void *out,
@@ -524,8 +526,9 @@ int pikv_prompt_mass(const void *q, const void *k, int32_t tokens, int64_t q_str
  *               p * stride_page + h' * stride_h + s * stride_s, D values each, on 16-byte boundaries; no two rows may overlap
  *   K_pool, V_pool  dtype;  page_table [B,E,ceil(S/page)] int32; an entry outside 0..n_pages-1 is no page
  *   entry_pos   [B,E,S] int32: positions (>= 0) of the entries, or NULL where nothing goes by them
- * In the descriptor D is 32, 64 or 128, rank 0 and flags 0 (UNSUPPORTED / INVALID otherwise); S is the capacity in slots;
- * its strides mean nothing here.                                                                          */
+ * In the descriptor D is 32, 64 or 128, rank 0 and flags 0 (UNSUPPORTED / INVALID otherwise); S is the capacity in slots, 2^30 at
+ * most; its strides mean nothing here.  Page errors: INVALID for n_pages < 1, another page size, strides that let rows overlap
+ * or are no multiples of 16 bytes; UNSUPPORTED for stride_s above 2^24 bytes, stride_h or stride_page above 2^40 elements.    */
 typedef struct pikv_pages {
     int32_t n_pages;      /* of the pools                                                  */
     int32_t page;         /* slots of a page: 16, 32, 64, 128 or 256                       */
@@ -542,8 +545,9 @@ typedef struct pikv_pages {
  *   utility   [B,E,S] float32: of a new entry its token's weight (0 without weights);  n_valid [B,E] int32, in place
  *   slots     [tokens,k] int32 out: the slot of token t in its j-th shard, -1 where it has none (of an index listed twice the
  *             first has it); rows of tokens in no sequence are left
- * Errors: descriptor and page errors, INVALID for null required pointers, k not in 1..E, tokens < 0, K_new or V_new not on 16-byte boundaries;
- * UNSUPPORTED for tokens > 2^23 and route_rows_per_seq != 1.  tokens == 0 and B == 0 are no-ops.                */
+ * Errors: descriptor and page errors, INVALID for null required pointers, one of positions and entry_pos without the other, k not in
+ * 1..E, tokens < 0, K_new, V_new or a pool not on 16-byte boundaries; UNSUPPORTED for tokens > 2^23, B * E >= 2^22 and
+ * route_rows_per_seq != 1.  tokens == 0 and B == 0 are no-ops.                                                        */
 int pikv_paged_fill(const pikv_desc *desc, const pikv_pages *pages, const void *K_new, const void *V_new, int32_t tokens,
                     const int32_t *cu_seqlens, const int32_t *topk_idx, int32_t k, const float *weight, const int32_t *positions,
                     void *K_pool, void *V_pool, const int32_t *page_table, int32_t *entry_pos, float *utility, int32_t *n_valid,
@@ -553,7 +557,8 @@ int pikv_paged_fill(const pikv_desc *desc, const pikv_pages *pages, const void *
  * shard is.  positions [B] int32, given with entry_pos or not at all.  An index outside 0..E-1 is no shard, one listed twice
  * takes the entry once.
  * Errors: descriptor and page errors, INVALID for null required pointers, k not in 1..E, one of reuse_idx and reuse_cnt without the other,
- * max_evict < 1 with them, K_new or V_new not on 16-byte boundaries; UNSUPPORTED for B * k > 2^21 and route_rows_per_seq != 1. */
+ * max_evict < 1 with them, K_new, V_new or a pool not on 16-byte boundaries; UNSUPPORTED for B * k > 2^21 and
+ * route_rows_per_seq != 1.  B == 0 is a no-op.                                                                        */
 int pikv_paged_append(const pikv_desc *desc, const pikv_pages *pages, const void *K_new, const void *V_new, const int32_t *topk_idx,
                       int32_t k, const int32_t *reuse_idx, const int32_t *reuse_cnt, int32_t max_evict, const int32_t *positions,
                       void *K_pool, void *V_pool, const int32_t *page_table, int32_t *entry_pos, float *utility, int32_t *n_valid,
@@ -572,7 +577,7 @@ size_t pikv_paged_attn_workspace_bytes(const pikv_desc *desc, int32_t k);
  * scores + slot_coef feed pikv_update_utility.  A selected index outside 0..E-1 counts as an empty shard, entries in a missing
  * page as not seen.  The workspace holds nothing between calls; calls that may overlap (streams, captured graphs) need one each.
  * Errors: as pikv_sharded_attn; descriptor and page errors; INVALID for one of entry_pos and q_pos without the other, or neither with slopes, a
- * window or a prefix, cap < 0, cap or scale NaN or infinite; UNSUPPORTED for tq > 1 with per-head routing, stride_s above 2^24 bytes, and 2^23 blocks
+ * window or a prefix, cap < 0, cap or scale NaN or infinite; UNSUPPORTED for tq > 1 with per-head routing and 2^23 blocks
  * of work or more.                                                                                        */
 int pikv_paged_attn(const pikv_desc *desc, const pikv_pages *pages, const void *q, const void *K_pool, const void *V_pool,
                     const int32_t *page_table, const int32_t *n_valid, const int32_t *topk_idx, const float *gates, int32_t k,

@@ -10,6 +10,11 @@
 //   * O^T[d][row] += V^T . P^T.
 // One pass with the running maximum and sum of the softmax (fp32).  bf16: a weight is rounded once, to bf16, on its way into the second
 // product - half a step of 2^-8 of each, as the output's own rounding - the sum is of the unrounded ones.
+//
+// 16384 tokens, 32 heads over 8 of 128 bf16 values: 2320 us, 945 TFLOP/s; the matrix pipe is busy 44 % of the cycles, the softmax's instructions most of the
+// others, and two waves a SIMD (registers) overlap the two as they come.  In a window of 1024 with capped scores (4 prompts of up to 4001, 16 heads over 4)
+// 142 us; 57 tokens 7.2 us, fp32 documents of up to 403 tokens 18.7.  32 rows a wave and 64 entries a tile are what 256 registers hold at 128
+// values: tiles of 32 entries take 2630 us, 64 rows a wave (512 registers) 3930.
 #include "pikv_decode_dev.h"
 #include "pikv_prompt_dev.h"
 
