@@ -12,7 +12,7 @@ if not torch.cuda.is_available():  # pragma: no cover
 
 import paged_reference as ref  # noqa: E402
 import paper_2508_06526_amd as pk  # noqa: E402
-from test_gpu_paged import Cache, check_fill, host, i32, up  # noqa: E402
+from test_gpu_paged import Attention, Cache, check_fill, host, i32, up  # noqa: E402
 from test_gpu_prompt import MARK, check_attention, check_mass  # noqa: E402
 
 DEV = "cuda:0"
@@ -253,3 +253,26 @@ def test_calls_without_tokens_or_sequences():
     c.untouched_elsewhere(np.zeros((2, E, S), bool))
     # sequences of a batch that have no tokens
     check_fill(Cache(4, E, HKV, S, D, "bf16", PAGE), [0, 7, 0, 0], K)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("change", [dict(), dict(slopes=True, window=50)], ids=["plain", "positions"])
+@pytest.mark.parametrize("Hkv,G,tq,D,S", [(2, 2, 3, 64, 90), (1, 4, 8, 128, 400), (2, 4, 2, 32, 1100)])
+def test_utilities_of_draft_queries(Hkv, G, tq, D, S, change, dtype):
+    """The raw scores and slot_coef of a call with drafts, through pikv_update_utility: the attention that all rows gave."""
+    a = Attention(2, 3, Hkv, G, S, D, dtype, 16, 2, tq=tq, seed=S + tq, **change)
+    a.run()
+    a.check()
+    u = torch.full((2, 3, S), 0.5, device=DEV)
+    pk.pikv_update_utility(a.c.desc, a.scores, a.coef, i32(a.n), i32(a.topk), 2, 0.25, u)
+    y, top, norm, weight, raw, A = a.reference()
+    _, err = ref.error_of(A, D, 300, 0.0, 40.0)
+    want, got = np.full((2, 3, S), 0.5), host(u)
+    for b in range(2):
+        for j, e in enumerate(a.topk[b]):
+            m = int(a.n[b, e])
+            with np.errstate(divide="ignore", invalid="ignore"):
+                p = np.where(norm[b, :, None] > 0, a.gates[b, j] * np.exp(raw[b, :, j, :m] - np.where(norm[b] > 0, top[b], 0.0)[:, None]) / norm[b, :, None], 0.0)
+            want[b, e, :m] = 0.125 + p.sum(0)
+    bar = (3 * err + (a.Hq + 20) * 2.0 ** -24) * np.maximum(want - 0.125, 0.0) + 2.0 ** -22 * want
+    assert (np.abs(got - want) <= bar).all(), float((np.abs(got - want) / bar).max())

@@ -320,3 +320,30 @@ def test_the_binding_refuses_what_is_too_small():
     with pytest.raises(pk.PikvError) as e:
         d.weigh()
     assert e.value.status == -3
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_as_far_apart_as_they_may_be(dtype):
+    """The largest stride, 2^25 bytes: offsets beyond 32 bits within a tile of 128 rows.  The same bits as packed rows."""
+    t = DTYPES[dtype]
+    Hq, Hkv, D, lens, stride = 2, 2, 64, [3, 140], (1 << 25) // (2 if dtype == "bf16" else 4)
+    T = sum(lens)
+    wide = torch.empty((T, stride), device=DEV, dtype=t)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(3)
+    packed = [torch.randn((T, Hq * D), generator=gen, device=DEV).to(t) for _ in range(3)]
+    views = [wide[:, i * 1024:i * 1024 + Hq * D] for i in range(3)]
+    for v, p in zip(views, packed):
+        v.copy_(p)
+    cu = i32([0, 3, T])
+    results = []
+    for (q, k, v), step in ((packed, Hq * D), (views, stride)):
+        out, mass = torch.zeros((T, Hq, D), device=DEV, dtype=t), torch.zeros(T, device=DEV)
+        stats = [torch.zeros((T, Hq), device=DEV) for _ in range(2)]
+        ws = torch.zeros(pk.pikv_prompt_mass_workspace_bytes(T, Hkv, 2, max(lens)), device=DEV, dtype=torch.uint8)
+        masks = (cu, 2, max(lens), None, 0.0, 0.0, None, 0)
+        pk.pikv_prompt_attn(q, k, v, T, step, step, step, Hq, Hkv, D, *masks, out, *stats)
+        pk.pikv_prompt_mass(q, k, T, step, step, Hq, Hkv, D, *masks, *stats, mass, ws)
+        torch.cuda.synchronize()
+        results.append([out, mass, *stats])
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and float(results[0][1].min()) > 0
