@@ -526,7 +526,8 @@ int pikv_prompt_mass(const void *q, const void *k, int32_t tokens, int64_t q_str
  *               p * stride_page + h' * stride_h + s * stride_s, D values each, on 16-byte boundaries; no two rows may overlap
  *   K_pool, V_pool  dtype;  page_table [B,E,ceil(S/page)] int32; an entry outside 0..n_pages-1 is no page
  *   entry_pos   [B,E,S] int32: positions (>= 0) of the entries, or NULL where nothing goes by them
- * In the descriptor D is 32, 64 or 128, rank 0 and flags 0 (UNSUPPORTED / INVALID otherwise); S is the capacity in slots, 2^30 at
+ * In the descriptor D is 32, 64 or 128, rank 0 and flags 0 (UNSUPPORTED / INVALID otherwise); Hq may be up to 1024 here, drafts of
+ * several tokens included (the utility updates take 256); S is the capacity in slots, 2^30 at
  * most; its strides mean nothing here.  Page errors: INVALID for n_pages < 1, another page size, strides that let rows overlap
  * or are no multiples of 16 bytes; UNSUPPORTED for stride_s above 2^24 bytes, stride_h or stride_page above 2^40 elements.    */
 typedef struct pikv_pages {

@@ -536,3 +536,19 @@ def test_the_binding_refuses_what_is_too_small():
     short[4] = args[4].float()
     with pytest.raises(TypeError):
         pk.pikv_paged_attn(*short)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("change", [dict(), dict(prefix=True, local=True)], ids=["plain", "prefix"])
+@pytest.mark.parametrize("Hkv,G,tq,S,D", [(8, 8, 5, 13, 128), (8, 8, 5, 300, 64), (4, 16, 16, 90, 32)])
+def test_more_query_rows_than_whole_shards_take(Hkv, G, tq, S, D, change, dtype):
+    a = Attention(2, 3, Hkv, G, S, D, dtype, 16, 2, tq=tq, seed=S, **change)
+    assert a.Hq > 256
+    a.run()
+    a.check()
+
+
+def test_routing_of_more_heads_than_whole_shards_take():
+    a = Attention(1, 4, 4, 80, 200, 64, "bf16", 16, 2, per_head=True, seed=3)
+    a.run()
+    a.check()

@@ -186,3 +186,13 @@ def test_strides_of_pages_beyond_the_offsets_of_the_kernels(lib, name):
     for value in (1 << 41, 1 << 61, 1 << 62):
         args = [FAKE] * 3, [2], [FAKE] * 2, [1], [FAKE] * 7, [None]
         assert lib.pikv_paged_append(*given(dict(g={"stride_page": 1 << 20, name: value})), *sum(args, [])) == UNSUPPORTED
+
+
+def test_query_rows_of_a_sequence(lib):
+    """Up to 1024 over pages, in every call on them."""
+    need = pk.pikv_paged_attn_workspace_bytes
+    for kw in (dict(Hq=320, Hkv=8, tq=5), dict(Hq=1024, Hkv=8), dict(Hq=1024, Hkv=256), dict(Hq=512, Hkv=1, route_rows_per_seq=512)):
+        assert need(desc(**kw), 2) > 0
+    for kw in (dict(Hq=1028), dict(Hq=512, Hkv=512), dict(Hq=322), dict(Hq=320, Hkv=8, tq=3), dict(Hq=320, route_rows_per_seq=32)):
+        assert need(desc(**kw), 2) == 0
+    assert lib.pikv_paged_append(*given(dict(d=dict(Hq=320, tq=5, B=0))), *sum(([FAKE] * 3, [2], [FAKE] * 2, [1], [FAKE] * 7, [None]), [])) == 0
