@@ -413,7 +413,7 @@ extern "C" int pikv_prompt_attn(const void *q, const void *k, const void *v, int
     p.v_stride = v_stride;
     p.unit = slopes ? 1.0f : cap > 0.0f ? cap : p.scale;
     p.unit_log2 = p.unit * 1.44269504088896340736f;
-    p.margin = 8.0f / p.unit_log2;
+    p.margin = fminf(8.0f / p.unit_log2, 1e30f);     // (finite: the first maximum passes it)
     p.out = out;
     p.row_max = row_max;
     p.row_norm = row_norm;
