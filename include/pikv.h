@@ -513,7 +513,7 @@ size_t pikv_prompt_mass_workspace_bytes(int32_t tokens, int32_t Hkv, int32_t B, 
  * they are inputs here.  A row whose row_norm is 0 gives nothing.
  *   mass      [tokens] float32 out
  * Sums run in a fixed order.  The workspace holds nothing between calls; calls that may overlap need one each.
- * Errors: as pikv_prompt_attn; WORKSPACE if workspace_bytes is too small.                                              */
+ * Errors: as pikv_prompt_attn; UNSUPPORTED for B * ceil(max_len / 64) >= 2^23 too; WORKSPACE if workspace_bytes is too small. */
 int pikv_prompt_mass(const void *q, const void *k, int32_t tokens, int64_t q_stride, int64_t k_stride, int32_t Hq, int32_t Hkv,
                      int32_t D, int32_t dtype, const int32_t *cu_seqlens, int32_t B, int32_t max_len, const int32_t *prefix,
                      float scale, float cap, const float *slopes, int32_t window, const float *row_max, const float *row_norm,

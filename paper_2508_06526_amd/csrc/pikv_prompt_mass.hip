@@ -291,6 +291,8 @@ extern "C" int pikv_prompt_mass(const void *q, const void *k, int32_t tokens, in
     const int64_t tiles = entry_tiles(max_len, kWaves * 32 * (dtype == PIKV_F32 ? sets_of<float> : sets_of<bf16>)), blocks = (int64_t)B * Hkv * tiles;
     const int runs = runs_of(B, Hkv, max_len);
     if ((int64_t)B * Hkv * prompt_tiles((int64_t)max_len * (Hq / Hkv)) >= (1 << 23) || blocks * runs >= (1 << 23)) return PIKV_ERR_UNSUPPORTED;
+    const int64_t joins = B * entry_tiles(max_len, kWave);
+    if (joins * kJoinThreads >= (int64_t)1 << 32) return PIKV_ERR_UNSUPPORTED;       // (threads of a launch)
     if (tokens == 0 || B == 0 || max_len == 0) return PIKV_OK;
     if (!q || !k || !cu_seqlens || !row_max || !row_norm || !mass) return PIKV_ERR_INVALID;
     if (!workspace || workspace_bytes < pikv_prompt_mass_workspace_bytes(tokens, Hkv, B, max_len)) return PIKV_ERR_WORKSPACE;
@@ -327,6 +329,6 @@ extern "C" int pikv_prompt_mass(const void *q, const void *k, int32_t tokens, in
     else by_width(bf16{});
     int done = launch_status();
     if (done != PIKV_OK || runs * Hkv == 1) return done;
-    hipLaunchKernelGGL(mass_join, dim3((unsigned)(B * (((int64_t)max_len + kWave - 1) / kWave))), dim3(kJoinThreads), 0, st, p);
+    hipLaunchKernelGGL(mass_join, dim3((unsigned)joins), dim3(kJoinThreads), 0, st, p);
     return launch_status();
 }

@@ -351,7 +351,7 @@ def test_rows_as_far_apart_as_they_may_be(dtype):
 
 @pytest.mark.parametrize("lens,Hq", [([200], 2), ([300] * 12, 16)], ids=["split", "whole"])
 def test_a_scale_that_leaves_nothing_of_the_scores(lens, Hq):
-    d = Device(ref.Prompts(lens, Hq, Hq, 128, "bf16", seed=4, scale=1e-38))
+    d = Device(Prompts(lens, Hq, Hq, 128, "bf16", seed=4, scale=1e-38))
     d.attend()
     check_attention(d)
     assert (host(d.row_norm) >= 1).all()

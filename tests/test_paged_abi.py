@@ -196,3 +196,10 @@ def test_query_rows_of_a_sequence(lib):
     for kw in (dict(Hq=1028), dict(Hq=512, Hkv=512), dict(Hq=322), dict(Hq=320, Hkv=8, tq=3), dict(Hq=320, route_rows_per_seq=32)):
         assert need(desc(**kw), 2) == 0
     assert lib.pikv_paged_append(*given(dict(d=dict(Hq=320, tq=5, B=0))), *sum(([FAKE] * 3, [2], [FAKE] * 2, [1], [FAKE] * 7, [None]), [])) == 0
+
+
+def test_no_launch_of_the_utilities_has_too_many_threads(lib):
+    """One head: 2^23 blocks of the sums' last step would be refused by the launch, after the first one has run."""
+    one = dict(Hq=1, Hkv=1, q_stride=64, k_stride=64, tokens=1 << 23, max_len=1 << 23)
+    assert mass(lib, B=64, **one) == UNSUPPORTED
+    assert mass(lib, B=64, ws=None, **dict(one, max_len=(1 << 23) - 64)) == WORKSPACE       # (the next smaller one gets past these checks)
