@@ -25,10 +25,11 @@ constexpr int kWaveRows = 32;            // rows of a wave
 // Waves of a block of many rows.  (8 waves halve the way of a tile into LDS for each row, and wait for each other: 16384 tokens of 128 values 2269 us
 // against 2325, of 64 values 1681 against 1363, 16 x 1024 tokens 240 against 219, ragged prompts in a window 167 against 153.)
 constexpr int kWaves = 4;
+constexpr int kMostWaves = 8;            // of a block that splits the tiles of its rows
 
 // LDS tiles of KEYS entries x D values, in 16-byte chunks, a row's chunks exchanged by an xor so that the reads of a wave spread over
 // the banks: K is read as one chunk of 32 entries each, V (bf16) as 64 bytes of 4 neighbouring entries each.
-template <typename T, int D, bool SPLIT>
+template <typename T, int D, int SPLIT>
 struct Tile {
     static constexpr int KEYS = sizeof(T) == 2 && !SPLIT ? 64 : 32;
     static constexpr int THREADS = SPLIT ? kWave : kWaves * kWave;    // that bring a tile
@@ -47,12 +48,12 @@ __device__ __forceinline__ uint2 read_transposed(const void *at) {
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)at));
 }
 
-// CAP: scores capped by a tanh; BIAS: with a distance term.  SPLIT: for few rows, a block takes 32 of them and its waves every fourth tile each, by
+// CAP: scores capped by a tanh; BIAS: with a distance term.  SPLIT: for few rows, a block takes 32 of them and its waves every SPLIT-th tile each, by
 // themselves; their results are joined at the end.
-template <typename T, int D, bool CAP, bool BIAS, bool SPLIT>
-__global__ __launch_bounds__(kWaves *kWave, (SPLIT && D == 128 ? 1 : 2)) void prompt_attn(PromptParams p) {
+template <typename T, int D, bool CAP, bool BIAS, int SPLIT>
+__global__ __launch_bounds__((SPLIT ? SPLIT : kWaves) * kWave, (SPLIT == kWaves && D == 128 ? 1 : 2)) void prompt_attn(PromptParams p) {
     typedef Tile<T, D, SPLIT> L;
-    constexpr int WAVES = kWaves, ROWS = SPLIT ? kWaveRows : WAVES * kWaveRows, THREADS = L::THREADS;
+    constexpr int WAVES = SPLIT ? SPLIT : kWaves, ROWS = SPLIT ? kWaveRows : WAVES * kWaveRows, THREADS = L::THREADS;
     constexpr bool BF = sizeof(T) == 2;
     constexpr int KEYS = L::KEYS, KB = KEYS / 32, DT = D / 32, BUFFERS = SPLIT ? WAVES : 2, STEP = SPLIT ? WAVES : 1;
     constexpr int QN = D * (int)sizeof(T) / 32;                       // 16-byte pieces of a lane's query
@@ -326,7 +327,7 @@ __global__ __launch_bounds__(kWaves *kWave, (SPLIT && D == 128 ? 1 : 2)) void pr
         }
     };
     if constexpr (SPLIT) {
-        // the waves' accumulators over their tiles in LDS; each wave joins a quarter of them
+        // the waves' accumulators over their tiles in LDS; each wave joins its part of them
         constexpr int N = DT * 16, MINE = N / WAVES;
         static_assert(WAVES * N * kWave * 4 <= (int)(sizeof(Ks) + sizeof(Vs)) && N % WAVES == 0, "joined where the tiles were");
         __shared__ float base_s[WAVES][kWaveRows], l_s[WAVES][kWaveRows], top_s[WAVES][kWaveRows];
@@ -388,6 +389,14 @@ bool splits(int dtype, int D, int max_len, int64_t blocks) {
     return max_len > 32 && blocks <= (max_len > 128 ? most : most / 3);
 }
 
+// Waves of such a block: 8 (and their tiles) take a CU of their own, which up to 256 blocks have.  us, 4 waves and 8, one prompt of 200 / 400 / 1000 /
+// 2500 tokens in some 250 blocks - bf16, 128 values 9.4 : 9.4 (140 blocks), 11.5 : 10.2 (130), 18.3 : 15.0, 34.1 : 25.0; 64 values 6.6 : 6.7, 8.0 : 7.4, 12.3 :
+// 10.4, 23.0 : 17.2; fp32, 64 values 10.9 : 11.3, 16.0 : 15.5, 28.1 : 26.3, 60.6 : 54.1; in 416 blocks bf16, 64 values 8.7 : 11.6, 13.1 : 14.2 (400, 1000).  fp32 tiles of 128
+// values are too large for 8, of 32 values there are too few accumulators to join.
+int split_waves(int dtype, int D, int max_len, int64_t blocks) {
+    return blocks <= 256 && max_len > 256 && D >= 64 && D * elem_bytes(dtype) <= 256 ? kMostWaves : kWaves;
+}
+
 }  // namespace
 }  // namespace pikv
 
@@ -406,6 +415,7 @@ extern "C" int pikv_prompt_attn(const void *q, const void *k, const void *v, int
     const bool split = splits(dtype, D, max_len, (int64_t)B * Hkv * tiles_of(kWaves * kWaveRows));
     const int64_t tiles = tiles_of(split ? kWaveRows : kWaves * kWaveRows);
     if ((int64_t)B * Hkv * tiles >= (1 << 23)) return PIKV_ERR_UNSUPPORTED;
+    const int waves = !split ? 0 : split_waves(dtype, D, max_len, (int64_t)B * Hkv * tiles);
     if (tokens == 0 || B == 0 || max_len == 0) return PIKV_OK;       // (tensors without elements have no address)
     if (!q || !k || !v || !cu_seqlens || !out || reinterpret_cast<uintptr_t>(out) % 16 != 0) return PIKV_ERR_INVALID;
     PromptParams p = prompt_params(q, k, tokens, q_stride, k_stride, Hq, Hkv, D, cu_seqlens, B, max_len, prefix, scale, cap, slopes, window);
@@ -420,15 +430,21 @@ extern "C" int pikv_prompt_attn(const void *q, const void *k, const void *v, int
     p.by_head = fast_div(Hkv);
     p.by_tile = fast_div(B);
     p.tiles = (int)tiles;
-    const dim3 grid((unsigned)(B * Hkv * tiles)), threads(kWaves * kWave);
+    const dim3 grid((unsigned)(B * Hkv * tiles)), threads((waves > 0 ? waves : kWaves) * kWave);
     hipStream_t st = as_stream(stream);
     auto launch = [&](auto type, auto width) {
         typedef decltype(type) T;
         constexpr int W = decltype(width)::value;
         auto go = [&](auto capped, auto biased) {
             constexpr bool CAP = decltype(capped)::value, BIAS = decltype(biased)::value;
-            if (split) hipLaunchKernelGGL((prompt_attn<T, W, CAP, BIAS, true>), grid, threads, 0, st, p);
-            else hipLaunchKernelGGL((prompt_attn<T, W, CAP, BIAS, false>), grid, threads, 0, st, p);
+            if constexpr (W >= 64 && W * sizeof(T) <= 256) {
+                if (waves == kMostWaves) {
+                    hipLaunchKernelGGL((prompt_attn<T, W, CAP, BIAS, kMostWaves>), grid, threads, 0, st, p);
+                    return;
+                }
+            }
+            if (waves > 0) hipLaunchKernelGGL((prompt_attn<T, W, CAP, BIAS, kWaves>), grid, threads, 0, st, p);
+            else hipLaunchKernelGGL((prompt_attn<T, W, CAP, BIAS, 0>), grid, threads, 0, st, p);
         };
         const std::true_type yes{};
         const std::false_type no{};
