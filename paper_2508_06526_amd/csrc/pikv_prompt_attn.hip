@@ -229,7 +229,9 @@ __global__ __launch_bounds__((SPLIT ? SPLIT : kWaves) * kWave, (SPLIT == kWaves 
                 for (int i = 0; i < 16; ++i) most = fmaxf(most, s[kb][i]);
             top = fmaxf(top, most);
             if (__any(most > base + p.margin)) {
-                const float now = halves_max(fmaxf(top, base)), next_shift = now == -INFINITY ? 0.0f : now;
+                // (rows of which this holds: the others keep theirs, so that no row's roundings hang on those beside it)
+                const float highest = halves_max(fmaxf(top, base)), now = highest > base + p.margin ? highest : base;
+                const float next_shift = now == -INFINITY ? 0.0f : now;
                 const float corr = __builtin_amdgcn_exp2f((base - next_shift) * to_log2);
                 base = now;
                 shift = next_shift;
