@@ -8,7 +8,9 @@
 namespace pikv {
 
 // tanh x.  Small, for |x| < 1/2: x + x^3 P(x^2), P of degree 4 through tanh's values at the nodes of Chebyshev's polynomial over that range (off by
-// 1.04 * 2^-24 of the value, roundings included).  Large: from exp(2 |x|), off by some 2^-23 whatever the value.
+// 1.04 * 2^-24 of the value, roundings included).  Large, for the others: from exp(2 |x|), off by at most 3.6 * 2^-24 - of the exponential 1.4, of the
+// sum and its reciprocal 1.6, of the result 0.5 -, which is less than 2^-21 of these values.
+constexpr float kTanhSmall = 0.5f;
 __device__ __forceinline__ float tanh_small(float x) {
     const float y = x * x;
     float t = -0.0069470033f;
@@ -19,11 +21,11 @@ __device__ __forceinline__ float tanh_small(float x) {
     return fmaf(t * y, x, x);
 }
 __device__ __forceinline__ float tanh_large(float x) {
-    const float e = __expf(2.0f * fabsf(x));         // (infinite: 1)
+    const float e = __builtin_amdgcn_exp2f(fabsf(x) * 2.88539008177792681472f);      // (2 log2 e; infinite: 1)
     return copysignf(fmaf(-2.0f, __builtin_amdgcn_rcpf(e + 1.0f), 1.0f), x);
 }
-// N products to parts of a cap, tanh(dot * by), by = scale / cap.  Where a wave holds one that is large, all of them are taken for such: off by
-// 2^-23 of the cap, which is 2^-22 of that score.
+// N products to parts of a cap, tanh(dot * by), by = scale / cap.  Each score takes its own form: neither what is not seen nor another row of the wave
+// has a part in its bits.  The larger form is only entered where a wave holds a score that needs it.
 template <int N>
 __device__ __forceinline__ void cap_parts(float (&s)[N], float by) {
     float most = 0.0f;
@@ -32,9 +34,9 @@ __device__ __forceinline__ void cap_parts(float (&s)[N], float by) {
         s[i] *= by;
         most = fmaxf(most, fabsf(s[i]));
     }
-    if (__any(most >= 0.5f)) {
+    if (__any(most >= kTanhSmall)) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] = tanh_large(s[i]);
+        for (int i = 0; i < N; ++i) s[i] = fabsf(s[i]) < kTanhSmall ? tanh_small(s[i]) : tanh_large(s[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) s[i] = tanh_small(s[i]);
