@@ -481,7 +481,8 @@ int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t block, const 
  *     s = scale <q_i, k_j>;   cap > 0: s = cap tanh(s / cap);   slopes: s = s - slopes[h] |p_i - p_j|
  * and j is seen by i where  p_j < prefix  or  (p_j <= p_i and (window <= 0 or p_i - p_j < window)); a prefix is seen by all
  * tokens of its sequence, window or not (its own among them: both ways), what is not seen has weight zero, whatever it
- * holds.  scale <= 0 selects 1/sqrt(D).
+ * holds.  scale <= 0 selects 1/sqrt(D).  Factors have to be float32 numbers: where 1 / cap or scale / cap is beyond them (a cap below some
+ * 3e-39), the calls are UNSUPPORTED.
  *
  * Prompts are packed: the tokens of sequence b are rows cu_seqlens[b] .. cu_seqlens[b+1]-1 of [tokens, ...] arrays, their positions
  * count from 0, and no sequence sees another.  Rows in no sequence, and those of a sequence from max_len on, are neither read nor
@@ -497,8 +498,8 @@ int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t block, const 
  * Errors: INVALID for null required pointers, one of row_max and row_norm without the other, tokens, B or max_len < 0, Hq or
  * Hkv < 1, Hq % Hkv != 0, strides or
  * addresses as above, cap < 0, cap or scale NaN or infinite, unknown dtype; UNSUPPORTED for D other than 32, 64, 128, Hq > 256, a
- * stride above 2^25 bytes, tokens > 2^23 or 2^23 blocks of work and more (128 rows of a kv head's queries each, B times those of the
- * longest sequence).  tokens == 0, B == 0 and max_len == 0 are no-ops.                                                 */
+ * stride above 2^25 bytes, tokens > 2^23, 2^23 blocks of work and more (128 rows of a kv head's queries each, B times those of the
+ * longest sequence), and, here alone, without slopes a cap or an uncapped scale above 2.3e38 (the scores' unit times log2 e).  tokens == 0, B == 0 and max_len == 0 are no-ops.                                                 */
 int pikv_prompt_attn(const void *q, const void *k, const void *v, int32_t tokens, int64_t q_stride, int64_t k_stride,
                      int64_t v_stride, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype, const int32_t *cu_seqlens, int32_t B,
                      int32_t max_len, const int32_t *prefix, float scale, float cap, const float *slopes, int32_t window, void *out,

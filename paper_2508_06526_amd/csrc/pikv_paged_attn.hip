@@ -589,6 +589,7 @@ extern "C" int pikv_paged_attn(const pikv_desc *desc, const pikv_pages *pages, c
     if (rc != PIKV_OK) return rc;
     if (combine != PIKV_COMBINE_LSE && combine != PIKV_COMBINE_LOCAL) return PIKV_ERR_INVALID;
     if (!(scale - scale == 0.0f) || !(cap >= 0.0f) || !(cap - cap == 0.0f)) return PIKV_ERR_INVALID;
+    if (!score_factors_finite(scale, desc->D, cap)) return PIKV_ERR_UNSUPPORTED;
     if ((entry_pos != nullptr) != (q_pos != nullptr) || ((slopes || window > 0 || prefix) && !entry_pos && desc->B > 0)) return PIKV_ERR_INVALID;
     if (desc->B == 0) return PIKV_OK;            // (tensors without elements have no address)
     if (!q || !K_pool || !V_pool || !page_table || !n_valid || !topk_idx || !y) return PIKV_ERR_INVALID;
@@ -629,7 +630,7 @@ extern "C" int pikv_paged_attn(const pikv_desc *desc, const pikv_pages *pages, c
     p.chunk = plan.chunk;
     p.window = window;
     p.nsplit_rcp = plan.nsplit > 1 ? (uint32_t)(((uint64_t)1 << 32) / plan.nsplit + 1) : 0u;
-    p.scale = scale > 0.0f ? scale : 1.0f / sqrtf((float)desc->D);
+    p.scale = score_scale(scale, desc->D);
     p.cap = cap;
     p.cap_rcp = cap > 0.0f ? 1.0f / cap : 0.0f;
     p.shard_waves = kMergedWaves / k;

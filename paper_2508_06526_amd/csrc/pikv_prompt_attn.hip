@@ -411,6 +411,8 @@ extern "C" int pikv_prompt_attn(const void *q, const void *k, const void *v, int
     const int rc = check_prompt(q, k, v, true, tokens, q_stride, k_stride, v_stride, Hq, Hkv, D, dtype, B, max_len, scale, cap);
     if (rc != PIKV_OK) return rc;
     if ((row_max != nullptr) != (row_norm != nullptr)) return PIKV_ERR_INVALID;
+    const float unit = slopes ? 1.0f : cap > 0.0f ? cap : score_scale(scale, D), unit_log2 = unit * 1.44269504088896340736f;
+    if (!(unit_log2 - unit_log2 == 0.0f)) return PIKV_ERR_UNSUPPORTED;
     if (max_len > tokens) max_len = tokens;
     const int G = Hq / Hkv;
     auto tiles_of = [&](int block_rows) { return ((int64_t)max_len * G + block_rows - 1) / block_rows; };
@@ -423,8 +425,8 @@ extern "C" int pikv_prompt_attn(const void *q, const void *k, const void *v, int
     PromptParams p = prompt_params(q, k, tokens, q_stride, k_stride, Hq, Hkv, D, cu_seqlens, B, max_len, prefix, scale, cap, slopes, window);
     p.v = v;
     p.v_stride = v_stride;
-    p.unit = slopes ? 1.0f : cap > 0.0f ? cap : p.scale;
-    p.unit_log2 = p.unit * 1.44269504088896340736f;
+    p.unit = unit;
+    p.unit_log2 = unit_log2;
     p.margin = fminf(8.0f / p.unit_log2, 1e30f);     // (finite: the first maximum passes it)
     p.out = out;
     p.row_max = row_max;

@@ -76,6 +76,7 @@ inline int check_prompt(const void *q, const void *k, const void *v, bool values
     if (dtype != PIKV_F32 && dtype != PIKV_BF16) return PIKV_ERR_INVALID;
     if (!(scale - scale == 0.0f) || !(cap >= 0.0f) || !(cap - cap == 0.0f)) return PIKV_ERR_INVALID;
     if ((D != 32 && D != 64 && D != 128) || Hq > 256 || tokens > (1 << 23)) return PIKV_ERR_UNSUPPORTED;
+    if (!score_factors_finite(scale, D, cap)) return PIKV_ERR_UNSUPPORTED;
     const int es = elem_bytes(dtype);
     auto rows = [&](const void *p, int64_t stride, int heads) {
         return stride >= (int64_t)heads * D && stride * es % 16 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
@@ -106,7 +107,7 @@ inline PromptParams prompt_params(const void *q, const void *k, int tokens, int6
     p.Hkv = Hkv;
     p.B = B;
     p.window = window;
-    p.scale = scale > 0.0f ? scale : 1.0f / sqrtf((float)D);
+    p.scale = score_scale(scale, D);
     p.cap = cap;
     p.cap_rcp = cap > 0.0f ? 1.0f / cap : 0.0f;
     return p;

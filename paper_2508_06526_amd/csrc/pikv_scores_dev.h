@@ -1,4 +1,4 @@
-// Capped scores: cap tanh(s / cap).
+// Capped scores: cap tanh(s / cap).  What a call may give for cap and scale.
 #pragma once
 
 #include "pikv_common.h"
@@ -6,6 +6,14 @@
 #include <math.h>
 
 namespace pikv {
+
+// Host: a scale of a call as the kernels take it, and whether their factors are finite: an infinite one makes a NaN of a product that is zero.
+inline float score_scale(float scale, int D) { return scale > 0.0f ? scale : 1.0f / sqrtf((float)D); }
+inline bool score_factors_finite(float scale, int D, float cap) {
+    if (cap == 0.0f) return true;
+    const float rcp = 1.0f / cap, by = score_scale(scale, D) * rcp;
+    return rcp - rcp == 0.0f && by - by == 0.0f;
+}
 
 // tanh x.  Small, for |x| < 1/2: x + x^3 P(x^2), P of degree 4 through tanh's values at the nodes of Chebyshev's polynomial over that range (off by
 // 1.04 * 2^-24 of the value, roundings included).  Large, for the others: from exp(2 |x|), off by at most 3.6 * 2^-24 - of the exponential 1.4, of the
