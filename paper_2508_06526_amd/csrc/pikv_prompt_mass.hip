@@ -41,6 +41,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
     // of a tile's rows: maximum, 1 / sum (0: gives nothing), token, slope
     __shared__ __attribute__((aligned(16))) float row_max_s[2][ROWS], weight_s[2][ROWS], slope_s[2][BIAS ? ROWS : 4];
     __shared__ __attribute__((aligned(16))) int token_s[2][ROWS];
+    __shared__ int none_s[2];            // a row of the tile gives nothing
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, h = lane >> 5;
     int hk, b, split;
@@ -108,6 +109,8 @@ __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
             row_max_s[buffer][tid] = norm_r == 0.0f ? INFINITY : max_r;
             weight_s[buffer][tid] = norm_r == 0.0f ? 0.0f : 1.0f / norm_r;
             token_s[buffer][tid] = token_r;
+            const bool none = __any(norm_r == 0.0f) != 0;        // (one wave)
+            if (tid == 0) none_s[buffer] = none;
             if constexpr (BIAS) slope_s[buffer][tid] = slope_r;
         }
     };
@@ -127,7 +130,8 @@ __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
             const int first_token = row_token(p, row0), last_token = row_token(p, min(row0 + ROWS, to) - 1);
             const bool any = wave_entry < n && (wave_entry < prefix || (wave_entry <= last_token && (p.window <= 0 || first_token - (wave_entry + ENTRIES - 1) < p.window)));
             if (any) {
-                const bool masked = !(wave_entry + ENTRIES <= prefix || (wave_entry + ENTRIES - 1 <= first_token &&
+                // (a row that gives nothing may hold anything, scores that are no numbers among them: it is masked)
+                const bool masked = __builtin_amdgcn_readfirstlane(none_s[buffer]) != 0 || !(wave_entry + ENTRIES <= prefix || (wave_entry + ENTRIES - 1 <= first_token &&
                                                                           (p.window <= 0 || last_token - wave_entry < p.window))) || row0 + ROWS > to;
                 const uint32_t q_at = opaque(L::chunk(c, h) * 16 + buffer * (int)sizeof(Qs[0]));
                 const uint32_t reach = p.window > 0 ? p.window : 0x80000000u;
@@ -196,7 +200,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_partial(PromptParams p) {
                                     float e = __builtin_amdgcn_exp2f(v * kLog2e), weight = ws[x];        // (0: top is infinite)
                                     if constexpr (MASKED) {      // (both: what is not seen may hold anything)
                                         // (no short circuits: they become branches)
-                                        const bool seen = ((uint32_t)(tokens[x] - entry) < reach) | (entry < prefix);
+                                        const bool seen = (((uint32_t)(tokens[x] - entry) < reach) | (entry < prefix)) & (ws[x] != 0.0f);
                                         e = seen ? e : 0.0f;
                                         weight = seen ? weight : 0.0f;
                                     }
