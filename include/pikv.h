@@ -576,7 +576,7 @@ size_t pikv_paged_attn_workspace_bytes(const pikv_desc *desc, int32_t k);
  * Where slopes, a window or a prefix is given, entry_pos and q_pos are too; where entry_pos is given, entries that a query does not
  * see (later ones among them: drafts that have been appended see each other causally) have the score -inf, and
  * an entry with a negative position is seen by none.  Without entry_pos every valid entry is seen.
- * scores + slot_coef feed pikv_update_utility.  A selected index outside 0..E-1 counts as an empty shard, entries in a missing
+ * scores + slot_coef feed pikv_update_utility.  The float32 outputs may start at any float's address.  A selected index outside 0..E-1 counts as an empty shard, entries in a missing
  * page as not seen.  The workspace holds nothing between calls; calls that may overlap (streams, captured graphs) need one each.
  * Errors: as pikv_sharded_attn; descriptor and page errors; INVALID for one of entry_pos and q_pos without the other, or neither with slopes, a
  * window or a prefix, cap < 0, cap or scale NaN or infinite; UNSUPPORTED for tq > 1 with per-head routing and 2^23 blocks

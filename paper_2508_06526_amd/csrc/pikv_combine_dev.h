@@ -231,8 +231,7 @@ __device__ __forceinline__ void combine_weights_block(const CombineParams &p, in
         if (mine) {
             shard_w[tid] = hw.w;
             if (p.slot_coef)
-                *reinterpret_cast<float2 *>(p.slot_coef + ((int64_t)bh * p.k + tid) * 2) =
-                    make_float2(hw.shift, hw.coef);
+                store_floats(p.slot_coef + ((int64_t)bh * p.k + tid) * 2, make_float2(hw.shift, hw.coef));
         }
         if (tid == 0) {
             if (p.row_max) p.row_max[out] = hw.M;
@@ -266,7 +265,7 @@ __device__ __forceinline__ void combine_weights_wave(const CombineParams &p, int
     for (int s = sub + 8 * kShardPairsHeld; s < nsplit; s += 8) wt[j * p.nsplit + s] = weight(pair(s));
     if (writes) {
         if (p.slot_coef && j < p.k && sub == 0)
-            *reinterpret_cast<float2 *>(p.slot_coef + ((int64_t)bh * p.k + j) * 2) = make_float2(hw.shift, hw.coef);
+            store_floats(p.slot_coef + ((int64_t)bh * p.k + j) * 2, make_float2(hw.shift, hw.coef));
         if (lane == 0) {
             if (p.row_max) p.row_max[out] = hw.M;
             if (p.row_norm) p.row_norm[out] = hw.norm;
@@ -397,7 +396,7 @@ __device__ __forceinline__ void combine_head(const CombineParams &p, int bh, uns
         if (cgroups <= 8) t = add4(t, other(t, std::integral_constant<int, 3>{}));
         if (cgroups <= 4) t = add4(t, other(t, std::integral_constant<int, 2>{}));
         if (p.rank == 0) {
-            if (lane < cgroups) *reinterpret_cast<float4 *>(p.y + out * p.D + lane * 4) = t;
+            if (lane < cgroups) store_floats(p.y + out * p.D + lane * 4, t);
             return;
         }
         if (lane < cgroups) *reinterpret_cast<float4 *>(ycode + lane * 4) = t;

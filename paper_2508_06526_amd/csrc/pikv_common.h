@@ -155,6 +155,15 @@ typedef u32x4_t __attribute__((address_space(1))) *global_u32x4_wptr;
 __device__ __forceinline__ void store16(void *p, uint4 v) {
     *(u32x4_t __attribute__((address_space(1))) *)(uintptr_t)p = u32x4_t{v.x, v.y, v.z, v.w};
 }
+// Neighbouring floats of an array that a caller may give at any float's address: the same instructions, which ask for no more than that.
+__device__ __forceinline__ void store_floats(float *p, float4 v) {
+    typedef float any_float4 __attribute__((ext_vector_type(4), aligned(4)));
+    *(any_float4 __attribute__((address_space(1))) *)(uintptr_t)p = any_float4{v.x, v.y, v.z, v.w};
+}
+__device__ __forceinline__ void store_floats(float *p, float2 v) {
+    typedef float any_float2 __attribute__((ext_vector_type(2), aligned(4)));
+    *(any_float2 __attribute__((address_space(1))) *)(uintptr_t)p = any_float2{v.x, v.y};
+}
 __device__ __forceinline__ void store16_stream(void *p, uint4 v) {
     const u32x4_t x = {v.x, v.y, v.z, v.w};
     __builtin_nontemporal_store(x, (global_u32x4_wptr)(uintptr_t)p);

@@ -256,8 +256,7 @@ __global__ __launch_bounds__(WAVES *kWave, WAVES == kWaves ? quant_blocks_per_cu
                     for (int hb = 0; hb < 2; ++hb) {
                         const int at = t0 + 16 * hb + 4 * r;
                         if (at + 4 <= last && (p.S & 3) == 0) {
-                            store16(to + at, make_uint4(__float_as_uint(sv[rt][4 * hb]), __float_as_uint(sv[rt][4 * hb + 1]),
-                                                        __float_as_uint(sv[rt][4 * hb + 2]), __float_as_uint(sv[rt][4 * hb + 3])));
+                            store_floats(to + at, make_float4(sv[rt][4 * hb], sv[rt][4 * hb + 1], sv[rt][4 * hb + 2], sv[rt][4 * hb + 3]));
                         } else {
 #pragma unroll
                             for (int x = 0; x < 4; ++x)
