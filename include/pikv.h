@@ -522,14 +522,15 @@ int pikv_prompt_mass(const void *q, const void *k, int32_t tokens, int64_t q_str
 
 /* A paged cache: slot i of shard (b, e) lies in page page_table[b][e][i / page], at slot i % page of it; pages are parts of one
  * pool of K rows and one of V rows, which shards of other requests may share.  Slots keep their numbers, so pikv_route, pikv_evict
- * with compact == 0, the pikv_policy calls and the utility updates serve such a cache as they are.
+ * with compact == 0, the pikv_policy calls and the utility updates serve such a cache as they are; what pikv_append does for whole shards,
+ * the refill of evicted slots included, pikv_paged_append does for these.
  *   pikv_pages  geometry of both pools, in elements: page p, kv head h', slot s of it start at
  *               p * stride_page + h' * stride_h + s * stride_s, D values each, on 16-byte boundaries; no two rows may overlap
  *   K_pool, V_pool  dtype;  page_table [B,E,ceil(S/page)] int32; an entry outside 0..n_pages-1 is no page
  *   entry_pos   [B,E,S] int32: positions (>= 0) of the entries, or NULL where nothing goes by them
- * In the descriptor D is 32, 64 or 128, rank 0 and flags 0 (UNSUPPORTED / INVALID otherwise); Hq may be up to 1024 here, drafts of
- * several tokens included (the utility updates take 256); S is the capacity in slots, 2^30 at
- * most; its strides mean nothing here.  Page errors: INVALID for n_pages < 1, another page size, strides that let rows overlap
+ * In the descriptor D is 32, 64 or 128, rank 0 and flags 0 (UNSUPPORTED / INVALID otherwise); Hq may be up to 1024 here and where an
+ * eviction without compaction or a policy call takes the same descriptor, drafts of several tokens included (the utility updates take 256);
+ * S is the capacity in slots, 2^30 at most; its strides mean nothing to the calls on pages (the others want valid ones, as of whole shards).  Page errors: INVALID for n_pages < 1, another page size, strides that let rows overlap
  * or are no multiples of 16 bytes; UNSUPPORTED for stride_s above 2^24 bytes, stride_h or stride_page above 2^40 elements.    */
 typedef struct pikv_pages {
     int32_t n_pages;      /* of the pools                                                  */

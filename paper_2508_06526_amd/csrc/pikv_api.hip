@@ -25,6 +25,16 @@ int check_desc(const pikv_desc *d, bool eight_bit) {
     return PIKV_OK;
 }
 
+int check_slots(const pikv_desc *d, bool eight_bit) {
+    if (!d) return PIKV_ERR_INVALID;
+    pikv_desc few = *d;                  // (a query row of each kv head)
+    if (d->Hq > 256 && d->Hq <= kPagedRows && d->Hkv > 0 && d->Hq % d->Hkv == 0) {
+        few.Hq = d->Hkv;
+        if (d->route_rows_per_seq == d->Hq) few.route_rows_per_seq = few.Hq;
+    }
+    return check_desc(&few, eight_bit);
+}
+
 }  // namespace pikv
 
 extern "C" const char *pikv_strerror(int status) {

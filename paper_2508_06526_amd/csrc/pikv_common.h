@@ -234,6 +234,10 @@ inline int launch_status() { return hipGetLastError() == hipSuccess ? PIKV_OK : 
 // Host-side descriptor checks common to every call that takes a pikv_desc.  A call that reads or writes rows of the dense type refuses the
 // descriptor of an 8-bit cache; `eight_bit`: the call serves that too.
 int check_desc(const pikv_desc *d, bool eight_bit = false);
+// The same for the calls that go by slots and counts alone, and those on pages: nothing there is laid out by the query rows of a sequence, up to
+// kPagedRows with drafts of several tokens.
+constexpr int kPagedRows = 1024;
+int check_slots(const pikv_desc *d, bool eight_bit);
 inline int desc_width(const pikv_desc *d) { return d->rank ? d->rank : d->D; }
 inline int elem_bytes(int dtype) { return dtype == PIKV_F32 ? 4 : 2; }
 

@@ -630,7 +630,7 @@ extern "C" int pikv_evict(const pikv_desc *desc, float *utility, int32_t *n_vali
                           int32_t *evicted_idx, int32_t *evicted_cnt, int32_t max_evict,
                           int32_t compact, void *const *K_shards, void *const *V_shards,
                           void *stream) {
-    const int rc = check_desc(desc, !compact);
+    const int rc = compact ? check_desc(desc) : check_slots(desc, true);
     if (rc != PIKV_OK) return rc;
     if (!utility || !n_valid || !evicted_idx || !evicted_cnt) return PIKV_ERR_INVALID;
     if (capacity < 0 || max_evict < 1) return PIKV_ERR_INVALID;

@@ -5,21 +5,14 @@
 
 namespace pikv {
 
-constexpr int kPagedRows = 1024;         // query rows of a sequence, at most
-
 // What the calls on paged shards check of their descriptor (its strides mean nothing there) and of the pages.
 inline int check_paged(const pikv_desc *d, const pikv_pages *pages) {
     if (!d || !pages) return PIKV_ERR_INVALID;
     pikv_desc whole = *d;
     whole.stride_s = d->rank > 0 ? d->rank : d->D;
     whole.stride_h = (int64_t)(d->S > 0 ? d->S : 1) * whole.stride_s;
-    // (nothing here is laid out by the query rows of a sequence: drafts of several tokens make them more than other calls take)
     if (d->Hq > kPagedRows) return PIKV_ERR_UNSUPPORTED;
-    if (d->Hq > 256 && d->Hkv > 0 && d->Hq % d->Hkv == 0) {
-        whole.Hq = d->Hkv;
-        if (d->route_rows_per_seq == d->Hq) whole.route_rows_per_seq = whole.Hq;
-    }
-    const int rc = check_desc(&whole);
+    const int rc = check_slots(&whole, false);
     if (rc != PIKV_OK) return rc;
     if (d->rank != 0 || d->D < 32 || d->S > (1 << 30)) return PIKV_ERR_UNSUPPORTED;
     if (pages->n_pages < 1) return PIKV_ERR_INVALID;
