@@ -493,7 +493,9 @@ int pikv_quant_attn(const pikv_desc *desc, int32_t format, int32_t block, const 
  *             row, multiples of 16 bytes; heads are D apart), on 16-byte boundaries
  *   cu_seqlens [B+1] int32, ascending, within 0..tokens;  max_len: the longest sequence, or more
  *   prefix    [B] int32 or NULL;  slopes [Hq] float32 or NULL
- *   out       [tokens, Hq, D] dtype out: rows go on into a projection of the storage type
+ *   out       [tokens, Hq, D] dtype out: rows go on into a projection of the storage type.  bf16: the weights exp(s_j - shift) are rounded to
+ *             bf16 for their product with v, which is off by up to 2^-8 sum_j p_j |v_j| beside the output's own rounding; row_max, row_norm and the
+ *             sum that out is divided by are of the unrounded ones
  *   row_max, row_norm [tokens, Hq] float32 out or both NULL: the largest score of the row and sum_j exp(s_j - row_max)
  * Errors: INVALID for null required pointers, one of row_max and row_norm without the other, tokens, B or max_len < 0, Hq or
  * Hkv < 1, Hq % Hkv != 0, strides or
@@ -542,6 +544,9 @@ typedef struct pikv_pages {
  * shard (b, e) the tokens of sequence b that list e take the slots from n_valid[b][e] on, in their order.  If there are more of them than
  * the shard has room for - up to S, and to its first missing page - those of the largest weight stay (equal ones: the earlier token; a NaN
  * ranks below all; without weights the earliest), in the tokens' order: Section 3.4's bounded memory, without a row written that goes at once.
+ * What a shard holds already stays, whatever its utility: a full shard takes nothing.  Slots from n_valid on count as free, so the
+ * holes of a pikv_evict are refilled first (pikv_paged_append, reuse_idx): behind an eviction alone the fill would write over the entry that
+ * lies at n_valid and leave the evicted one in its place.
  *   K_new, V_new [tokens,Hkv,D] dtype;  cu_seqlens [B+1] as above
  *   topk_idx  [tokens,k] int32: an index outside 0..E-1 is no shard, one listed twice takes the entry once
  *   weight    [tokens] float32 or NULL;  positions [tokens] int32, given with entry_pos or not at all
@@ -577,8 +582,10 @@ size_t pikv_paged_attn_workspace_bytes(const pikv_desc *desc, int32_t k);
  * Where slopes, a window or a prefix is given, entry_pos and q_pos are too; where entry_pos is given, entries that a query does not
  * see (later ones among them: drafts that have been appended see each other causally) have the score -inf, and
  * an entry with a negative position is seen by none.  Without entry_pos every valid entry is seen.
- * scores + slot_coef feed pikv_update_utility.  The float32 outputs may start at any float's address.  A selected index outside 0..E-1 counts as an empty shard, entries in a missing
- * page as not seen.  The workspace holds nothing between calls; calls that may overlap (streams, captured graphs) need one each.
+ * scores + slot_coef feed pikv_update_utility.  The float32 outputs may start at any float's address.  A selected index outside 0..E-1
+ * counts as an empty shard, entries in a missing page as not seen.  A row with a score that is no number is NaN in y; its row_norm and
+ * slot_coef leave out the parts of the shards that hold one, as pikv_sharded_attn's do (pikv_prompt_attn's row_norm is NaN then).
+ * The workspace holds nothing between calls; calls that may overlap (streams, captured graphs) need one each.
  * Errors: as pikv_sharded_attn; descriptor and page errors; INVALID for one of entry_pos and q_pos without the other, or neither with slopes, a
  * window or a prefix, cap < 0, cap or scale NaN or infinite; UNSUPPORTED for tq > 1 with per-head routing and 2^23 blocks
  * of work or more.                                                                                        */

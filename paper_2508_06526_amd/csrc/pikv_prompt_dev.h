@@ -23,7 +23,8 @@ struct PromptParams {
     float unit, unit_log2, margin;      // pikv_prompt_attn: of the scores as they are kept
 };
 
-// row / G for 0 <= row < 2^31 / G: rows of a kv head are (token, head of the group).
+// row / G for 0 <= row < 2^31: rows of a kv head are (token, head of the group).  (G_rcp is at most 2^32 / G + 1: for such rows the product is the
+// quotient or one more.)
 __device__ __forceinline__ int row_token(const PromptParams &p, int row) {
     if (p.G == 1) return row;
     int t = (int)__umulhi((uint32_t)row, p.G_rcp);

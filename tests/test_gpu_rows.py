@@ -54,3 +54,19 @@ def test_rows_of_a_step(G, D, S, dtype):
     same = np.arange(a.Hq) % G != 0
     for got, w in zip((b.y, b.row_max, b.row_norm), want):
         np.testing.assert_array_equal(host(got)[:, same], w[:, same])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G,D,S", [(4, 64, 100), (16, 128, 700), (33, 32, 300), (4, 64, 6000)])
+def test_a_query_that_is_no_number(G, D, S, dtype):
+    """NaN in its own row of y, nothing of it in row_norm and slot_coef, and no other row any different - in one launch and in two."""
+    make = lambda: Attention(2, 3, 2, G, S, D, dtype, 16, 2, seed=4, full=True)
+    a, b = make(), make()
+    a.run()
+    b.q[1, G - 1, 3] = np.nan
+    b.run()
+    other = np.ones(a.y.shape[:2], bool)
+    other[1, G - 1] = False
+    for got, w in zip((b.y, b.row_max, b.row_norm, b.coef), (a.y, a.row_max, a.row_norm, a.coef)):
+        np.testing.assert_array_equal(host(got)[other], host(w)[other])
+    assert np.isnan(host(b.y)[~other]).all() and (host(b.row_norm)[~other] == 0).all() and (host(b.coef)[~other][..., 1] == 0).all()
