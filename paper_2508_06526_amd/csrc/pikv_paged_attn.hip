@@ -15,7 +15,7 @@
 // its own; requests go out a stage ahead through buffer descriptors that end with the last entry.
 //
 // Bound by the rows: 128 MiB (a sequence, 4 shards of 8192 slots, 32 heads over 8 of 128 bf16 values, raw scores written) 22.8 us, 5.9 TB/s, and the merge
-// 4.5; 296 MB of 32 ragged sequences with capped scores and a distance bias 63 us in one launch, 4.7 TB/s.
+// 4.5; 296 MB of 32 ragged sequences with capped scores and a distance bias 61 - 67 us in one launch, by the card, 4.4 - 4.9 TB/s.
 #include "pikv_combine_dev.h"
 #include "pikv_decode_dev.h"
 #include "pikv_mfma_dev.h"

@@ -9,11 +9,13 @@
 //     entries in the same order (bf16: transposing reads of 4 entries from LDS).
 //   * O^T[d][row] += V^T . P^T.
 // One pass with the running maximum and sum of the softmax (fp32).  bf16: a weight is rounded once, to bf16, on its way into the second
-// product - half a step of 2^-8 of each, as the output's own rounding - the sum is of the unrounded ones.
+// product - half a step of 2^-8 of each, as the output's own rounding - the sum is of the unrounded ones.  (Two parts instead, 16 bits: error
+// against 64 bits 0.0021 -> 0.0016 of the values, which is the output's rounding alone, and half as many products again: 16384 tokens 2250 -> 2970 us, in a
+// window 147 -> 168.)
 //
-// 16384 tokens, 32 heads over 8 of 128 bf16 values: 2320 us, 945 TFLOP/s; the matrix pipe is busy 44 % of the cycles, the softmax's instructions most of the
+// 16384 tokens, 32 heads over 8 of 128 bf16 values: 2240 - 2450 us by the card, 900 - 980 TFLOP/s; the matrix pipe is busy 44 % of the cycles, the softmax's instructions most of the
 // others, and two waves a SIMD (registers) overlap the two as they come.  In a window of 1024 with capped scores (4 prompts of up to 4001, 16 heads over 4)
-// 142 us; 57 tokens 7.2 us, fp32 documents of up to 403 tokens 18.7.  32 rows a wave and 64 entries a tile are what 256 registers hold at 128
+// 147 us; 57 tokens 7.3 us, fp32 documents of up to 403 tokens 20.7 (capped scores, each in the form for its size: 143 and 18.7 with one form for a wave).  32 rows a wave and 64 entries a tile are what 256 registers hold at 128
 // values: tiles of 32 entries take 2630 us, 64 rows a wave (512 registers) 3930.
 #include "pikv_decode_dev.h"
 #include "pikv_prompt_dev.h"

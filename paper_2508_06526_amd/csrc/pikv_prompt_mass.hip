@@ -7,7 +7,7 @@
 //                  and sums exp(s - row_max) / row_norm in its own registers, 32 rows at a time and then over them.
 //   mass_join    : the kv heads' sums (and those of the runs that few blocks' rows were cut into), in a fixed order.
 //
-// 8192 tokens, 32 heads over 8 of 128 bf16 values: 350 us, 790 TFLOP/s, the matrix pipe busy 39 % of the cycles: an exponential and three more vector
+// 8192 tokens, 32 heads over 8 of 128 bf16 values: 334 - 353 us by the card, 780 - 823 TFLOP/s, the matrix pipe busy 36 - 39 % of the cycles: an exponential and three more vector
 // operations for each score.  (32 entries a wave, which read a row's tile from LDS twice as often, in blocks of uneven length: 990 us; an address of its own
 // for each piece of a tile, 64 bits wide: 381.)
 #include "pikv_prompt_dev.h"
